@@ -21,6 +21,9 @@ BD_MODE_BIDIR, BD_MODE_CAUSAL = 0, 1
 BD_FLAG_CHIP_WIDE_HANDOVER, BD_FLAG_REGISTER_RING, BD_FLAG_PREFILL_DECODE, BD_FLAG_PREFILL_STAGED = 1, 2, 4, 8
 BD_FLAG_ATTENTION_KEY_SPLIT = 16
 BD_FLAG_MEASURE_NO_WEIGHTS = 32
+BD_KV8_PAGE, BD_KV8_BAD_ROWS, BD_KV8_BAD_PAGE = 32, 1, 2
+BD_ROPE_HALF, BD_ROPE_INTERLEAVED = 0, 1
+BD_ROPE_PLAIN, BD_ROPE_LINEAR, BD_ROPE_BASE, BD_ROPE_PARTS = 0, 1, 2, 3
 
 # every symbol the two headers declare
 EXPORTS = [
@@ -29,6 +32,7 @@ EXPORTS = [
     "bd_read_carry", "bd_read_rows", "bd_forward_bytes", "bd_strerror", "bd_last_error",
     "bd_k_attention", "bd_k_attention_static", "bd_k_profile", "bd_k_profile_read", "bd_k_class_count", "bd_k_class_name",
     "bd_k_class_bytes", "bd_k_trace", "bd_k_trace_read", "bd_k_stream_floor", "bd_kv_page_order", "bd_kv_pages", "bd_k_raise_device_error",
+    "bd_k_kv8_write", "bd_k_kv8_read", "bd_k_kv8_attention", "bd_k_kv8_attention_workspace", "bd_k_rope", "bd_k_rope_plan",
 ]
 
 
@@ -36,6 +40,15 @@ class bd_config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_layers", "hidden", "n_q_heads", "n_kv_heads", "head_dim", "ffn", "vocab")] + \
                [("rope_theta", C.c_float), ("rms_eps", C.c_float)] + \
                [(n, C.c_int32) for n in ("max_seq", "max_block", "mask_token_id", "weight_dtype", "flags")]
+
+
+class bd_kv8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dev_codes", "dev_scales", "dev_pages", "dev_len", "dev_status")] + \
+               [(n, C.c_int32) for n in ("n_pages", "n_kv", "D", "n_seq", "max_blocks")]
+
+
+class bd_rope(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("D", "rotary_dim", "layout")] + [("amplitude", C.c_float), ("inv_freq", C.c_double * 64)]
 
 
 _lib = None
@@ -90,6 +103,14 @@ def lib() -> C.CDLL:
     L.bd_k_raise_device_error.argtypes = [vp]
     L.bd_k_stream_floor.argtypes = [vp, i32, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
     L.bd_k_trace_read.argtypes = [vp, vp, i32, C.POINTER(i32), C.POINTER(i32)]
+    i64 = C.c_int64
+    L.bd_k_kv8_write.argtypes = [vp, vp, vp, i64, i64, vp, i64, i64, i32, i32, vp]
+    L.bd_k_kv8_read.argtypes = [vp, vp, vp, i32, vp, i32, vp, i64, i64, vp, i64, i64]
+    L.bd_k_kv8_attention.argtypes = [vp, vp, vp, i64, i64, i32, i32, vp, i32, i32, i32, f32, vp, i64, i64, vp, i64]
+    L.bd_k_kv8_attention_workspace.argtypes = [vp, i32, i32, i32, i32]
+    L.bd_k_kv8_attention_workspace.restype = i64
+    L.bd_k_rope_plan.argtypes = [vp, i32, i32, i32, C.c_double, i32, C.c_double, i32]
+    L.bd_k_rope.argtypes = [vp, vp, vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, vp, vp]
     _lib = L
     return L
 
@@ -329,4 +350,143 @@ def bd_k_attention_static(q, k, v, n_prefix: int, mode: int, out=None):
         out = torch.empty((M, n_q * D), dtype=torch.float32, device="cuda")
     _check(lib().bd_k_attention_static(C.c_void_p(torch.cuda.current_stream().cuda_stream), _ptr(q), _ptr(k), _ptr(v),
                                        n_prefix, M, n_q, n_kv, D, mode, _ptr(out)))
+    return out
+
+
+# -- attention on a key/value cache in 8 bits (include/bd_kernels.h) --------------------------------------------------------
+
+def _rows_of(t, name, heads, D, device):
+    """(pointer, stride between sequences, stride between rows) of a tensor of rows [n_seq, M, heads, D]."""
+    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != D:
+        raise ValueError(f"{name}: expected [n_seq, M, {heads}, {D}], got {list(t.shape)}")
+    n, m, _, _ = t.shape
+    s0, s1, s2, s3 = t.stride()
+    if s3 != 1 or (heads > 1 and s2 != D) or t.device != device:
+        raise ValueError(f"{name}: heads and dimensions have to be contiguous, on {device}")
+    return t.data_ptr(), s0 if n > 1 else 0, s1 if m > 1 else 0
+
+
+def _ints_of(t, name, n_seq, device):
+    """Pointer of an int32 tensor with one number for each sequence; None passes NULL."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.numel() != n_seq or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: expected {n_seq} int32 numbers on {device}")
+    return t.data_ptr()
+
+
+def _dtype_of(t, name):
+    import torch
+    if t.dtype == torch.bfloat16:
+        return BD_BF16
+    if t.dtype == torch.float32:
+        return BD_F32
+    raise ValueError(f"{name}: bfloat16 or float32, got {t.dtype}")
+
+
+def _enqueue(device, call, *args):
+    """call(stream, *args) on the device's current stream."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        _check(call(torch.cuda.current_stream(device).cuda_stream, *args))
+    else:
+        with torch.cuda.device(device):
+            _check(call(torch.cuda.current_stream(device).cuda_stream, *args))
+
+
+class Kv8Cache:
+    """A key/value cache in 8 bits: caller's tensors behind one bd_kv8.  Methods carry the names of the C calls they wrap.
+
+    codes uint8 [n_pages, n_kv, 64 D], scales int32 [n_pages, n_kv], pages int32 [n_seq, max_blocks], lens int32 [n_seq]
+    (positions held; moved on by the caller), status None or one int32.  The tensors are kept alive, and looked at when the kernels run."""
+
+    def __init__(self, codes, scales, pages, lens, status=None):
+        import torch
+        if codes.dtype != torch.uint8 or codes.dim() != 3 or not codes.is_cuda or not codes.is_contiguous():
+            raise ValueError("codes: expected a contiguous uint8 tensor [n_pages, n_kv, 64 D] on the GPU")
+        n_pages, n_kv, size = codes.shape
+        self.device = codes.device
+        if scales.dtype != torch.int32 or list(scales.shape) != [n_pages, n_kv] or not scales.is_contiguous() or scales.device != self.device:
+            raise ValueError(f"scales: expected a contiguous int32 tensor [{n_pages}, {n_kv}] on {self.device}")
+        if pages.dtype != torch.int32 or pages.dim() != 2 or not pages.is_contiguous() or pages.device != self.device:
+            raise ValueError(f"pages: expected a contiguous int32 tensor [n_seq, max_blocks] on {self.device}")
+        self.n_seq, self.n_kv, self.D = pages.shape[0], n_kv, size // 64
+        self._keep = (codes, scales, pages, lens, status)
+        self._c = bd_kv8(codes.data_ptr(), scales.data_ptr(), pages.data_ptr(), _ints_of(lens, "lens", self.n_seq, self.device),
+                         _ints_of(status, "status", 1, self.device), n_pages, n_kv, self.D if size % 64 == 0 else 0, self.n_seq, pages.shape[1])
+        self._p = C.addressof(self._c)
+
+    @staticmethod
+    def empty(n_pages, n_kv, D, pages, lens, status=None):
+        """A cache of n_pages pages that hold nothing yet."""
+        import torch
+        return Kv8Cache(torch.zeros((n_pages, n_kv, 64 * D), dtype=torch.uint8, device=pages.device),
+                        torch.zeros((n_pages, n_kv), dtype=torch.int32, device=pages.device), pages, lens, status)
+
+    def _batch(self, t, name):
+        if t.shape[0] != self.n_seq:
+            raise ValueError(f"{name}: {t.shape[0]} sequences, the cache has {self.n_seq}")
+        return t.shape[1]
+
+    def bd_k_kv8_write(self, k, v, rows=None):
+        """Keys and values [n_seq, M, n_kv, D] (bfloat16 or float32) to positions lens ..."""
+        kp, vp = _rows_of(k, "k", self.n_kv, self.D, self.device), _rows_of(v, "v", self.n_kv, self.D, self.device)
+        M = self._batch(k, "k")
+        if v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("k and v: same shape and type")
+        _enqueue(self.device, lib().bd_k_kv8_write, self._p, *kp, *vp, _dtype_of(k, "k"), M, _ints_of(rows, "rows", self.n_seq, self.device))
+
+    def bd_k_kv8_read(self, start, k_out, v_out, rows=None):
+        """Positions start .. (None: from 0) as values, to k_out and v_out [n_seq, M, n_kv, D]."""
+        kp, vp = _rows_of(k_out, "k_out", self.n_kv, self.D, self.device), _rows_of(v_out, "v_out", self.n_kv, self.D, self.device)
+        M = self._batch(k_out, "k_out")
+        if v_out.shape != k_out.shape or v_out.dtype != k_out.dtype:
+            raise ValueError("k_out and v_out: same shape and type")
+        _enqueue(self.device, lib().bd_k_kv8_read, self._p, _ints_of(start, "start", self.n_seq, self.device), M,
+                 _ints_of(rows, "rows", self.n_seq, self.device), _dtype_of(k_out, "k_out"), *kp, *vp)
+
+    def bd_k_kv8_attention_workspace(self, n_q, M, window=0, sinks=0) -> int:
+        return _check(lib().bd_k_kv8_attention_workspace(self._p, n_q, M, window, sinks))
+
+    def bd_k_kv8_attention(self, q, out, mode, window=0, sinks=0, scale=0.0, rows=None, workspace=None):
+        """Attention of q [n_seq, M, n_q, D] (bfloat16) on the cache, to out (same shape).  workspace: a uint8 tensor of
+        bd_k_kv8_attention_workspace bytes that nothing else uses while the call runs; None takes one from torch for this call."""
+        import torch
+        if q.dim() != 4 or q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape != q.shape:
+            raise ValueError("q and out: bfloat16 [n_seq, M, n_q, D], same shape")
+        n_q = q.shape[2]
+        qp, op = _rows_of(q, "q", n_q, self.D, self.device), _rows_of(out, "out", n_q, self.D, self.device)
+        M = self._batch(q, "q")
+        if workspace is None:
+            size = self.bd_k_kv8_attention_workspace(n_q, M, window, sinks)
+            workspace = torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous tensor on {self.device}")
+        wp, wn = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
+        _enqueue(self.device, lib().bd_k_kv8_attention, self._p, *qp, n_q, M, _ints_of(rows, "rows", self.n_seq, self.device), mode, window,
+                 sinks, scale, *op, wp, wn)
+        return out
+
+
+def bd_k_rope_plan(D, rotary_dim=None, layout=BD_ROPE_HALF, theta=1.0e6, scaling=BD_ROPE_PLAIN, factor=1.0, trained=1) -> bd_rope:
+    """Plan of rotary positions (see include/bd_kernels.h); rotary_dim None: the whole head."""
+    plan = bd_rope()
+    _check(lib().bd_k_rope_plan(C.addressof(plan), D, D if rotary_dim is None else rotary_dim, layout, theta, scaling, factor, trained))
+    return plan
+
+
+def bd_k_rope(plan, x, pos, out=None, rows=None):
+    """The rows x [n_seq, M, heads, D] turned by their positions pos[s] + row, to out (None: a new tensor; x itself: in place)."""
+    import torch
+    if x.dim() != 4:
+        raise ValueError(f"x: expected [n_seq, M, heads, D], got {list(x.shape)}")
+    n, M, heads, _ = x.shape
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if rows is None else torch.zeros(x.shape, dtype=x.dtype, device=x.device)
+    if not x.is_cuda or out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("x and out: same shape and type, on the GPU")
+    xp, op = _rows_of(x, "x", heads, plan.D, x.device), _rows_of(out, "out", heads, plan.D, x.device)
+    _enqueue(x.device, lib().bd_k_rope, C.addressof(plan), *xp, *op, _dtype_of(x, "x"), heads, n, M, _ints_of(pos, "pos", n, x.device),
+             _ints_of(rows, "rows", n, x.device))
     return out

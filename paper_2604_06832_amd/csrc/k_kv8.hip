@@ -1,0 +1,728 @@
+// Attention on a key/value cache in 8 bits, and what fills and reads it (include/bd_kernels.h: bd_rope, bd_kv8).
+#include <cmath>
+
+#include "kv8.h"
+#include "launch.h"
+#include "stream_fwd.h"
+
+namespace bd {
+namespace {
+
+typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+
+struct Kv8Rows {          // a call's rows: their positions and how many of each sequence are real
+  const int* first; const int* rows; int M;
+};
+
+// First position and number of rows of sequence s; false (and reported) where they make no sense.
+__device__ inline bool kv8_take(const bd_kv8& c, const Kv8Rows& r, int s, int& first, int& rows) {
+  first = r.first != nullptr ? r.first[s] : 0;
+  rows = r.rows != nullptr ? r.rows[s] : r.M;
+  if (kv8_rows_ok(first, rows, r.M, c.max_blocks)) return true;
+  if (c.dev_status != nullptr && threadIdx.x == 0) atomicOr(c.dev_status, BD_KV8_BAD_ROWS);
+  return false;
+}
+// Page of block kb of sequence s; -1 (and reported) where it lies outside the pool.
+__device__ inline int kv8_page(const bd_kv8& c, int s, int kb) {
+  const int page = c.dev_pages[(size_t)s * c.max_blocks + kb];
+  if ((unsigned)page < (unsigned)c.n_pages) return page;
+  if (c.dev_status != nullptr) atomicOr(c.dev_status, BD_KV8_BAD_PAGE);
+  return -1;
+}
+
+__device__ inline float two_to(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Four e4m3 codes of y (already scaled), to nearest, ties to even.
+__device__ inline uint32_t encode4(const float* y) {
+  float z[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) z[i] = fabsf(y[i]) > 448.f ? copysignf(448.f, y[i]) : y[i];   // (a NaN stays: the comparison is false)
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], w, true);
+}
+__device__ inline void decode4(uint32_t w, float* y) {
+  const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  y[0] = a[0]; y[1] = a[1]; y[2] = b[0]; y[3] = b[1];
+}
+
+template <typename T, int N> struct alignas(N * sizeof(T)) Pack { T x[N]; };
+template <typename T> __device__ inline float to_f32(T x);
+template <> __device__ inline float to_f32<float>(float x) { return x; }
+template <> __device__ inline float to_f32<u16>(u16 x) { return bf16_bits_to_f32(x); }
+template <typename T> __device__ inline T from_f32(float x);
+template <> __device__ inline float from_f32<float>(float x) { return x; }
+template <> __device__ inline u16 from_f32<u16>(float x) {
+  union { __bf16 h; u16 u; } v;                       // (the conversion keeps NaN and infinity)
+  v.h = (__bf16)x;
+  return v.u;
+}
+
+// ---- write --------------------------------------------------------------------------------------------------------------
+// One workgroup of 2 D threads per (touched block, head, keys or values).  A thread holds 16 of the block's elements in registers: of the keys
+// eight dimensions of two tokens (eight bytes of the page each), of the values eight tokens of two dimensions (likewise).
+// Bound by the rows' bytes; the block's maximum is one reduction over the workgroup between the load and the store.
+struct Kv8WriteArgs {
+  bd_kv8 c;
+  Kv8Rows r;
+  const void* x[2];
+  int64_t seq_stride[2], row_stride[2];                // of keys, of values
+};
+
+template <int D, typename T>
+__global__ __launch_bounds__(2 * D) void kv8_write_kernel(Kv8WriteArgs a) {
+  __shared__ uint32_t s_max[2 * D / 64], s_nan[2 * D / 64];
+  const int s = blockIdx.z, h = blockIdx.y >> 1, kv = blockIdx.y & 1;
+  int n, rows;
+  if (!kv8_take(a.c, a.r, s, n, rows)) return;
+  const int kb = n / 32 + blockIdx.x;
+  const int lo = max(n - kb * 32, 0), hi = min(n + rows - kb * 32, 32);     // tokens [lo, hi) of the block are new, those before stay
+  if (hi <= lo) return;
+  const int page = kv8_page(a.c, s, kb);
+  if (page < 0) return;
+  const size_t ph = (size_t)page * a.c.n_kv + h;
+  uint8_t* base = a.c.dev_codes + ph * (64 * D);
+  const int tid = threadIdx.x;
+  const int64_t row_stride = a.row_stride[kv];
+  const T* x = reinterpret_cast<const T*>(a.x[kv]) + s * a.seq_stride[kv] + (kb * 32 - n) * row_stride + h * D;
+  const int e_old = lo > 0 ? kv8_byte_exponent(a.c.dev_scales[ph] >> (8 * kv)) : kv8_e_min;
+  float y[2][8];
+  uint8_t* at[2];
+  int tok[2][2];                                       // first token of group j, and its step from element to element
+  if (kv == 0) {
+    const int d = (tid % (D / 8)) * 8;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int t = tid / (D / 8) + 16 * j;
+      tok[j][0] = t; tok[j][1] = 0;
+      at[j] = base + kv8_k_byte(t, d, D);
+      if (t >= lo && t < hi) {
+        constexpr int N = 16 / sizeof(T);
+#pragma unroll
+        for (int q = 0; q < 8 / N; ++q) {
+          const Pack<T, N> p = *reinterpret_cast<const Pack<T, N>*>(x + t * row_stride + d + q * N);
+#pragma unroll
+          for (int i = 0; i < N; ++i) y[j][q * N + i] = to_f32(p.x[i]);
+        }
+      }
+    }
+  } else {
+    const int d = (tid % (D / 2)) * 2, g = tid / (D / 2);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = 8 * g + i;
+      if (t >= lo && t < hi) {
+        const Pack<T, 2> p = *reinterpret_cast<const Pack<T, 2>*>(x + t * row_stride + d);
+        y[0][i] = to_f32(p.x[0]);
+        y[1][i] = to_f32(p.x[1]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      tok[j][0] = 8 * g; tok[j][1] = 1;
+      at[j] = base + 32 * D + kv8_v_byte(8 * g, d + j);
+    }
+  }
+  uint32_t amax = 0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = tok[j][0] + tok[j][1] * i;
+      const uint32_t u = __float_as_uint(y[j][i]) & 0x7FFFFFFFu;
+      if (t >= lo && t < hi && u < 0x7F800000u) amax = max(amax, u);        // (finite ones; their bits order them)
+    }
+#pragma unroll
+  for (int w = 32; w >= 1; w >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, w, 64));
+  if ((tid & 63) == 0) s_max[tid >> 6] = amax;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 2 * D / 64; ++w) amax = max(amax, s_max[w]);
+  const int e = max(kv8_exponent(amax), e_old);
+  const float down = two_to(-e), again = two_to(max(e_old - e, -126));      // (a smaller one would give 0 all the same)
+  bool nan = false;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    float old[8];
+    const bool any_old = tok[j][0] < lo;
+    if (any_old) {
+      const uint2 w = *reinterpret_cast<const uint2*>(at[j]);
+      decode4(w.x, old);
+      decode4(w.y, old + 4);
+    }
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = tok[j][0] + tok[j][1] * i;
+      z[i] = t >= hi ? 0.f : t >= lo ? y[j][i] * down : old[i] * again;
+      nan |= z[i] != z[i];
+    }
+    *reinterpret_cast<uint2*>(at[j]) = make_uint2(encode4(z), encode4(z + 4));
+  }
+  uint8_t* word = reinterpret_cast<uint8_t*>(a.c.dev_scales + ph);          // keys and values have bytes of their own
+  if (kv == 0) {
+    if (tid == 0) word[0] = (uint8_t)(e + 127);
+    return;
+  }
+  const unsigned long long b = __builtin_amdgcn_ballot_w64(nan);
+  if ((tid & 63) == 0) s_nan[tid >> 6] = b != 0ull;
+  __syncthreads();
+  if (tid == 0) {
+    uint32_t f = 0;
+#pragma unroll
+    for (int w = 0; w < 2 * D / 64; ++w) f |= s_nan[w];
+    word[1] = (uint8_t)(e + 127);
+    word[2] = (uint8_t)f;
+    word[3] = 0;
+  }
+}
+
+// ---- read ---------------------------------------------------------------------------------------------------------------
+struct Kv8ReadArgs {
+  bd_kv8 c;
+  Kv8Rows r;
+  void* x[2];
+  int64_t seq_stride[2], row_stride[2];
+};
+
+template <int D, typename T>
+__global__ __launch_bounds__(2 * D) void kv8_read_kernel(Kv8ReadArgs a) {
+  const int s = blockIdx.z, h = blockIdx.y >> 1, kv = blockIdx.y & 1;
+  int n, rows;
+  if (!kv8_take(a.c, a.r, s, n, rows)) return;
+  const int kb = n / 32 + blockIdx.x;
+  const int lo = max(n - kb * 32, 0), hi = min(n + rows - kb * 32, 32);
+  if (hi <= lo) return;
+  const int page = kv8_page(a.c, s, kb);
+  if (page < 0) return;
+  const size_t ph = (size_t)page * a.c.n_kv + h;
+  const uint8_t* base = a.c.dev_codes + ph * (64 * D);
+  const int tid = threadIdx.x;
+  const int64_t row_stride = a.row_stride[kv];
+  T* x = reinterpret_cast<T*>(a.x[kv]) + s * a.seq_stride[kv] + (kb * 32 - n) * row_stride + h * D;
+  const float up = two_to(kv8_byte_exponent(a.c.dev_scales[ph] >> (8 * kv)));
+  if (kv == 0) {
+    const int d = (tid % (D / 8)) * 8;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int t = tid / (D / 8) + 16 * j;
+      if (t < lo || t >= hi) continue;
+      const uint2 w = *reinterpret_cast<const uint2*>(base + kv8_k_byte(t, d, D));
+      float y[8];
+      decode4(w.x, y);
+      decode4(w.y, y + 4);
+      constexpr int N = 16 / sizeof(T);
+#pragma unroll
+      for (int q = 0; q < 8 / N; ++q) {
+        Pack<T, N> p;
+#pragma unroll
+        for (int i = 0; i < N; ++i) p.x[i] = from_f32<T>(y[q * N + i] * up);
+        *reinterpret_cast<Pack<T, N>*>(x + t * row_stride + d + q * N) = p;
+      }
+    }
+  } else {
+    const int d = (tid % (D / 2)) * 2, g = tid / (D / 2);
+    float y[2][8];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint2 w = *reinterpret_cast<const uint2*>(base + 32 * D + kv8_v_byte(8 * g, d + j));
+      decode4(w.x, y[j]);
+      decode4(w.y, y[j] + 4);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = 8 * g + i;
+      if (t < lo || t >= hi) continue;
+      Pack<T, 2> p;
+      p.x[0] = from_f32<T>(y[0][i] * up);
+      p.x[1] = from_f32<T>(y[1][i] * up);
+      *reinterpret_cast<Pack<T, 2>*>(x + t * row_stride + d) = p;
+    }
+  }
+}
+
+// ---- attention ----------------------------------------------------------------------------------------------------------
+struct Kv8AttnArgs {
+  bd_kv8 c;
+  Kv8Rows r;
+  const u16* q; u16* out;
+  int64_t q_seq, q_row, o_seq, o_row;
+  float* part;
+  int n_q, mode, window, sinks;
+  float c_log2;                 // scale * log2(e)
+  int tiles, groups, chunks;
+};
+constexpr float kv8_lowest = -3.0e38f;   // start of a running maximum: below every finite score, and finite itself
+
+// A block's codes, as the lanes load them, and its scale word.
+template <int D>
+struct Kv8Block {
+  uint4 k[2][D / 64], v[D / 32];
+  uint32_t word;
+};
+template <int D>
+__device__ inline void kv8_load(Kv8Block<D>& b, const bd_kv8& c, int page, int h, uint32_t word, int lane) {
+  const uint4* p = reinterpret_cast<const uint4*>(c.dev_codes + ((size_t)page * c.n_kv + h) * (64 * D)) + lane;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) b.k[t][j] = p[(t * (D / 64) + j) * 64];
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j) b.v[j] = p[(D / 32 + j) * 64];
+  b.word = word;
+}
+// Eight codes times 2^e as a bf16 operand (exact).
+__device__ inline bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
+  union { bf16x8 v; bf16x2 h[4]; } o;
+  o.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  o.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  o.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return o.v;
+}
+
+// One block of 32 keys against JT tiles of 16 columns.  S^T = K Q^T, so that a lane has eight scores of one column, and
+// O^T = V^T P^T.  The running maximum follows the scores only when one exceeds it by more than 2^8: weights up to 256 lose nothing.
+template <int D, int JT, bool MASKED>
+__device__ inline void kv8_block(const Kv8Block<D>& b, const bf16x8 (&qf)[JT][D / 32], f32x4 (&O)[JT][D / 16], float (&mrun)[JT], float (&lrun)[JT],
+                                 int kb, const int (&p)[JT], int end, const Kv8AttnArgs& a, int g, float c) {
+  constexpr int DT = D / 16;
+  const float ks = two_to(kv8_byte_exponent(b.word)), vs = two_to(kv8_byte_exponent(b.word >> 8));
+  f32x4 s[JT][2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt) s[jt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      const bf16x8 k0 = widen8(b.k[t][j].x, b.k[t][j].y, ks), k1 = widen8(b.k[t][j].z, b.k[t][j].w, ks);
+#pragma unroll
+      for (int jt = 0; jt < JT; ++jt) s[jt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[jt][2 * j], s[jt][t], 0, 0, 0);
+#pragma unroll
+      for (int jt = 0; jt < JT; ++jt) s[jt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[jt][2 * j + 1], s[jt][t], 0, 0, 0);
+    }
+  }
+  float cm[JT];
+  bool move = false;
+#pragma unroll
+  for (int jt = 0; jt < JT; ++jt) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (MASKED)
+        if (!kv8_sees(p[jt], kb * 32 + 8 * g + e, end, a.mode, a.window, a.sinks)) s[jt][e >> 2][e & 3] = -INFINITY;
+      m = fmaxf(m, s[jt][e >> 2][e & 3]);
+    }
+    cm[jt] = rows_max(m) * c;
+    move |= cm[jt] > mrun[jt] + 8.f;
+  }
+  if (__builtin_amdgcn_ballot_w64(move) != 0ull) {
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt) {
+      const float mnew = fmaxf(mrun[jt], cm[jt]);
+      const float alpha = __builtin_amdgcn_exp2f(mrun[jt] - mnew);
+      mrun[jt] = mnew;
+      lrun[jt] *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) O[jt][dt] *= alpha;
+    }
+  }
+  bf16x8 p8[JT];
+#pragma unroll
+  for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float w = __builtin_amdgcn_exp2f(fmaf(s[jt][e >> 2][e & 3], c, -mrun[jt]));      // (an invisible key's is 0)
+      lrun[jt] += w;
+      p8[jt][e] = (__bf16)w;      // rounded for the product: at most 2^-9 of a weight, independent from key to key
+    }
+  if (MASKED && (b.word & kv8_v_nan) != 0u) {
+    // A NaN among the values of a block that not every row sees all of: 0 times it would be NaN in rows that do not see it.  The product
+    // runs without them, and a second one counts for each row and dimension the visible NaN.
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        bf16x8 v = widen8(u ? b.v[j].z : b.v[j].x, u ? b.v[j].w : b.v[j].y, vs), one;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool bad = (float)v[e] != (float)v[e];
+          one[e] = bad ? (__bf16)1.f : (__bf16)0.f;
+          v[e] = bad ? (__bf16)0.f : v[e];
+        }
+#pragma unroll
+        for (int jt = 0; jt < JT; ++jt) {
+          bf16x8 seen;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) seen[e] = kv8_sees(p[jt], kb * 32 + 8 * g + e, end, a.mode, a.window, a.sinks) ? (__bf16)1.f : (__bf16)0.f;
+          const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          O[jt][2 * j + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p8[jt], O[jt][2 * j + u], 0, 0, 0);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) O[jt][2 * j + u][r] = count[r] > 0.f ? NAN : O[jt][2 * j + u][r];
+        }
+      }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j) {
+    const bf16x8 v0 = widen8(b.v[j].x, b.v[j].y, vs), v1 = widen8(b.v[j].z, b.v[j].w, vs);
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt) O[jt][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p8[jt], O[jt][2 * j], 0, 0, 0);
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt) O[jt][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p8[jt], O[jt][2 * j + 1], 0, 0, 0);
+  }
+}
+
+// Eight neighbouring dimensions of a column's result: [32 c + 8 g, + 8).
+__device__ inline void kv8_store(u16* o, const f32x4& a, const f32x4& b, float inv) {
+  union { bf16x8 v; uint4 u; } w;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) { w.v[r] = (__bf16)(a[r] * inv); w.v[4 + r] = (__bf16)(b[r] * inv); }
+  *reinterpret_cast<uint4*>(o) = w.u;
+}
+
+// A workgroup of four wavefronts takes JT tiles of a (sequence, kv head) and one of the chunks of their blocks: block number idx belongs to
+// chunk idx % chunks and in it to wavefront (idx / chunks) % 4.  The wavefronts merge through LDS; a group in one chunk stores its result, of several each
+// leaves an unnormalised partial, which kv8_merge_kernel sums in the order of the chunks.  The workgroups of the tiles of one chunk have
+// numbers that differ by multiples of 8: one XCD, whose L2 then serves all but the first.
+template <int D, int JT> constexpr int kv8_attn_lds() { return 4 * JT * ((D / 16) * 1024 + 2 * 64); }
+template <int D, int JT>
+__global__ __launch_bounds__(256, JT > 2 ? 1 : 2) void kv8_attn_kernel(Kv8AttnArgs a) {
+  constexpr int DT = D / 16, NW = 4;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  f32x4* sO = reinterpret_cast<f32x4*>(lds);                            // [NW][JT][DT][64]
+  float* sm = reinterpret_cast<float*>(lds + NW * JT * DT * 1024);      // [NW][JT][16]
+  float* sl = sm + NW * JT * 16;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+  const int unit = (blockIdx.x / (8 * a.groups)) * 8 + (blockIdx.x & 7), grp = (blockIdx.x >> 3) % a.groups;
+  if (unit >= a.c.n_seq * a.c.n_kv * a.chunks) return;
+  const int chunk = unit % a.chunks, h = (unit / a.chunks) % a.c.n_kv, s = unit / (a.chunks * a.c.n_kv);
+  int n, rows;
+  if (!kv8_take(a.c, a.r, s, n, rows)) return;
+  const int G = a.n_q / a.c.n_kv, cols = rows * G, c0 = grp * JT * 16;
+  if (c0 >= cols) return;
+  const int r0 = c0 / G, r1 = (min(c0 + JT * 16, cols) - 1) / G;
+  const Kv8Span sp = kv8_span(n, rows, r0, r1, a.mode, a.window, a.sinks);
+  const int used = kv8_chunks_used(sp.count, a.chunks);
+  if (chunk >= used) return;
+  bf16x8 qf[JT][D / 32];
+  f32x4 O[JT][DT];
+  float mrun[JT], lrun[JT];
+  int p[JT];
+#pragma unroll
+  for (int jt = 0; jt < JT; ++jt) {
+    const int cc = min(c0 + jt * 16 + col, cols - 1);                   // (columns past the last one repeat it and store nothing)
+    p[jt] = n + cc / G;
+    const u16* qp = a.q + s * a.q_seq + (cc / G) * a.q_row + (h * G + cc % G) * D + 16 * g;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      qf[jt][2 * j] = *reinterpret_cast<const bf16x8*>(qp + 64 * j);
+      qf[jt][2 * j + 1] = *reinterpret_cast<const bf16x8*>(qp + 64 * j + 8);
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) O[jt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    mrun[jt] = kv8_lowest;
+    lrun[jt] = 0.f;
+  }
+  const int step = NW * used, first = wave * used + chunk;
+  const int cnt = sp.count > first ? (sp.count - first + step - 1) / step : 0;
+  for (int base = 0; base < cnt; base += 64) {
+    // pages and scales of the next 64 blocks, one a lane
+    int my_page = -1;
+    uint32_t my_word = 0;
+    if (base + lane < cnt) {
+      const int idx = first + (base + lane) * step;
+      my_page = kv8_page(a.c, s, idx < sp.sink_blocks ? idx : sp.first_block + idx - sp.sink_blocks);
+      if (my_page >= 0) my_word = a.c.dev_scales[(size_t)my_page * a.c.n_kv + h];
+    }
+    const int todo = min(cnt - base, 64);
+    for (int i = 0; i < todo; ++i) {
+      const int page = __builtin_amdgcn_readlane(my_page, i);
+      if (page < 0) continue;
+      const int idx = first + (base + i) * step;
+      const bool sink = idx < sp.sink_blocks;
+      const int kb = sink ? idx : sp.first_block + idx - sp.sink_blocks;
+      Kv8Block<D> b;
+      kv8_load<D>(b, a.c, page, h, (uint32_t)__builtin_amdgcn_readlane((int)my_word, i), lane);
+      const bool clear = sink ? kb < sp.clear_sinks : kb >= sp.clear_lo && kb < sp.clear_hi;
+      if (clear) kv8_block<D, JT, false>(b, qf, O, mrun, lrun, kb, p, n + rows, a, g, a.c_log2);
+      else kv8_block<D, JT, true>(b, qf, O, mrun, lrun, kb, p, n + rows, a, g, a.c_log2);
+    }
+  }
+#pragma unroll
+  for (int jt = 0; jt < JT; ++jt) {
+    const float l = rows_sum(lrun[jt]);
+    if (g == 0) {
+      sm[(wave * JT + jt) * 16 + col] = mrun[jt];
+      sl[(wave * JT + jt) * 16 + col] = l;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) sO[((wave * JT + jt) * DT + dt) * 64 + lane] = O[jt][dt];
+  }
+  __syncthreads();
+  // wavefront w sums pairs of d-tiles w, w + 4, ..
+  for (int item = wave; item < JT * (DT / 2); item += NW) {
+    const int jt = item / (DT / 2), j = item % (DT / 2), cc = c0 + jt * 16 + col;
+    float m = kv8_lowest, f[NW], l = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, sm[(w * JT + jt) * 16 + col]);
+    f32x4 o0 = f32x4{0.f, 0.f, 0.f, 0.f}, o1 = o0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      f[w] = __builtin_amdgcn_exp2f(sm[(w * JT + jt) * 16 + col] - m);
+      l += sl[(w * JT + jt) * 16 + col] * f[w];
+      o0 += sO[((w * JT + jt) * DT + 2 * j) * 64 + lane] * f[w];
+      o1 += sO[((w * JT + jt) * DT + 2 * j + 1) * 64 + lane] * f[w];
+    }
+    if (used == 1) {
+      if (cc < cols) kv8_store(a.out + s * a.o_seq + (cc / G) * a.o_row + (h * G + cc % G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
+    } else if (c0 + jt * 16 < cols) {
+      float* pp = a.part + ((((int64_t)s * a.c.n_kv + h) * a.tiles + grp * JT + jt) * a.chunks + chunk) * (16 * D + 32);
+      *reinterpret_cast<f32x4*>(pp + (2 * j * 64 + lane) * 4) = o0;
+      *reinterpret_cast<f32x4*>(pp + ((2 * j + 1) * 64 + lane) * 4) = o1;
+      if (j == 0 && g == 0) {
+        pp[16 * D + col] = m;
+        pp[16 * D + 16 + col] = l;
+      }
+    }
+  }
+}
+
+// The chunks of a tile summed in their order: one wavefront per (sequence, kv head, tile, pair of d-tiles).
+template <int D>
+__global__ __launch_bounds__(64) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
+  const int lane = threadIdx.x, col = lane & 15, g = lane >> 4;
+  const int j = blockIdx.x % (D / 32), tile = (blockIdx.x / (D / 32)) % a.tiles, sh = blockIdx.x / (D / 32 * a.tiles);
+  const int h = sh % a.c.n_kv, s = sh / a.c.n_kv;
+  int n, rows;
+  if (!kv8_take(a.c, a.r, s, n, rows)) return;
+  const int G = a.n_q / a.c.n_kv, cols = rows * G, c0 = tile / JT * JT * 16, cc = tile * 16 + col;
+  if (tile * 16 >= cols) return;
+  const Kv8Span sp = kv8_span(n, rows, c0 / G, (min(c0 + JT * 16, cols) - 1) / G, a.mode, a.window, a.sinks);
+  const int used = kv8_chunks_used(sp.count, a.chunks);
+  if (used == 1) return;
+  const float* base = a.part + ((int64_t)sh * a.tiles + tile) * a.chunks * (16 * D + 32);
+  float m = kv8_lowest;
+  for (int c = 0; c < used; ++c) m = fmaxf(m, base[c * (16 * D + 32) + 16 * D + col]);
+  float l = 0.f;
+  f32x4 o0 = f32x4{0.f, 0.f, 0.f, 0.f}, o1 = o0;
+  for (int c = 0; c < used; ++c) {
+    const float* pp = base + c * (16 * D + 32);
+    const float f = __builtin_amdgcn_exp2f(pp[16 * D + col] - m);
+    l += pp[16 * D + 16 + col] * f;
+    o0 += *reinterpret_cast<const f32x4*>(pp + (2 * j * 64 + lane) * 4) * f;
+    o1 += *reinterpret_cast<const f32x4*>(pp + ((2 * j + 1) * 64 + lane) * 4) * f;
+  }
+  if (cc < cols) kv8_store(a.out + s * a.o_seq + (cc / G) * a.o_row + (h * G + cc % G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
+}
+
+// ---- rotary positions -----------------------------------------------------------------------------------------------------
+struct RopeArgs {
+  bd_rope plan;
+  const void* x; void* y;
+  int64_t x_seq, x_row, y_seq, y_row;
+  const int* pos; const int* rows;
+  int heads, M;
+};
+
+// One workgroup per row: sines and cosines of the row's angles once for all heads (fp64 up to the reduced angle: at position 2^20 an
+// angle in fp32 is off by up to 2^-5), then the heads, a pair at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+  __shared__ float s_cos[64], s_sin[64];
+  const int s = blockIdx.y, r = blockIdx.x;
+  const int rows = a.rows != nullptr ? a.rows[s] : a.M;
+  if (r >= rows) return;
+  const int R2 = a.plan.rotary_dim >> 1, D = a.plan.D, tid = threadIdx.x;
+  if (tid < R2) {
+    const double turns = ((double)a.pos[s] + r) * a.plan.inv_freq[tid] * 0.15915494309189533577;   // 1/(2 pi)
+    float sn, cs;
+    sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
+    s_cos[tid] = cs * a.plan.amplitude;
+    s_sin[tid] = sn * a.plan.amplitude;
+  }
+  __syncthreads();
+  const T* x = reinterpret_cast<const T*>(a.x) + s * a.x_seq + r * a.x_row;
+  T* y = reinterpret_cast<T*>(a.y) + s * a.y_seq + r * a.y_row;
+  const bool half = a.plan.layout == BD_ROPE_HALF;
+  for (int i = tid; i < a.heads * (D >> 1); i += 256) {
+    const int h = i / (D >> 1), j = i % (D >> 1);
+    if (j < R2) {
+      const int d0 = h * D + (half ? j : 2 * j), d1 = h * D + (half ? j + R2 : 2 * j + 1);
+      const float u = to_f32(x[d0]), v = to_f32(x[d1]), c = s_cos[j], sn = s_sin[j];
+      y[d0] = from_f32<T>(u * c - v * sn);
+      y[d1] = from_f32<T>(v * c + u * sn);
+    } else {
+      y[h * D + 2 * j] = x[h * D + 2 * j];
+      y[h * D + 2 * j + 1] = x[h * D + 2 * j + 1];
+    }
+  }
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------------------
+constexpr int kMaxRows = 1 << 22;
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int check_cache(const bd_kv8* c, int M, bool shape_only = false) {
+  if (c == nullptr) return BD_E_ARG;
+  if ((c->D != 64 && c->D != 128) || c->n_pages < 1 || c->n_kv < 1 || c->n_kv > 4096 || c->n_seq < 1 || c->n_seq > 65535 || c->max_blocks < 1 ||
+      c->max_blocks > (1 << 25) || M < 1 || M > kMaxRows)
+    return BD_E_ARG;
+  if (shape_only) return BD_OK;
+  if (c->dev_codes == nullptr || !aligned16(c->dev_codes) || c->dev_scales == nullptr || c->dev_pages == nullptr) return BD_E_ARG;
+  return BD_OK;
+}
+// Rows tensor: not null, 16-byte aligned, strides of whole 16 bytes, at least `least` elements (a row, where rows are written).
+int check_rows(const void* p, int dtype, int64_t seq_stride, int64_t row_stride, int n_seq, int M, int64_t least = 0) {
+  if (dtype != BD_BF16 && dtype != BD_F32) return BD_E_DTYPE;
+  const int64_t unit = dtype == BD_F32 ? 4 : 8;
+  if (p == nullptr || !aligned16(p)) return BD_E_ARG;
+  if (n_seq > 1 && (seq_stride < least || seq_stride % unit != 0)) return BD_E_ARG;
+  if (M > 1 && (row_stride < least || row_stride % unit != 0)) return BD_E_ARG;
+  return BD_OK;
+}
+
+// Blocks of 32 positions that M rows can touch.
+int blocks_of(int M, int max_blocks) {
+  const int b = (M + 62) / 32;
+  return b < max_blocks ? b : max_blocks;
+}
+
+template <typename A, typename K>
+int launch_blocks(hipStream_t s, K kernel, int D, const bd_kv8& c, int M, const A& a) {
+  hipLaunchKernelGGL(kernel, dim3(blocks_of(M, c.max_blocks), 2 * c.n_kv, c.n_seq), dim3(2 * D), 0, s, a);
+  return check_launch();
+}
+
+template <int D, int JT>
+int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
+  constexpr int lds = kv8_attn_lds<D, JT>();
+  if (lds > 65536) HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attn_kernel<D, JT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+  const int64_t units = (int64_t)a.c.n_seq * a.c.n_kv * p.chunks, grid = (units + 7) / 8 * 8 * p.groups;
+  if (grid >= (1 << 24)) return BD_E_ARG;               // (2^32 threads are one too many for a launch)
+  hipLaunchKernelGGL((kv8_attn_kernel<D, JT>), dim3((unsigned)grid), dim3(256), lds, s, a);
+  BD_TRY(check_launch());
+  if (p.chunks > 1) {
+    hipLaunchKernelGGL((kv8_merge_kernel<D>), dim3((unsigned)((int64_t)a.c.n_seq * a.c.n_kv * p.tiles * (D / 32))), dim3(64), 0, s, a, JT);
+    BD_TRY(check_launch());
+  }
+  return BD_OK;
+}
+
+int check_attn(const bd_kv8* c, int n_q, int M, int window, int sinks, bool shape_only, Kv8Plan* p) {
+  BD_TRY(check_cache(c, M, shape_only));
+  if (n_q < 1 || n_q > (1 << 16) || n_q % c->n_kv != 0 || window < 0 || sinks < 0) return BD_E_ARG;
+  *p = kv8_plan(c->n_seq, M, n_q, c->n_kv, c->D, c->max_blocks, window, sinks);
+  return BD_OK;
+}
+
+}  // namespace
+}  // namespace bd
+
+using namespace bd;
+
+extern "C" int bd_k_kv8_write(void* hip_stream, const bd_kv8* cache, const void* dev_k, int64_t k_seq_stride, int64_t k_row_stride, const void* dev_v,
+                              int64_t v_seq_stride, int64_t v_row_stride, int dtype, int M, const int32_t* dev_rows) {
+  BD_TRY(check_cache(cache, M));
+  BD_TRY(check_rows(dev_k, dtype, k_seq_stride, k_row_stride, cache->n_seq, M));
+  BD_TRY(check_rows(dev_v, dtype, v_seq_stride, v_row_stride, cache->n_seq, M));
+  if (cache->dev_len == nullptr) return BD_E_ARG;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const Kv8WriteArgs a{*cache, {cache->dev_len, dev_rows, M}, {dev_k, dev_v}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}};
+  if (cache->D == 128)
+    return dtype == BD_F32 ? launch_blocks(s, kv8_write_kernel<128, float>, 128, *cache, M, a) : launch_blocks(s, kv8_write_kernel<128, u16>, 128, *cache, M, a);
+  return dtype == BD_F32 ? launch_blocks(s, kv8_write_kernel<64, float>, 64, *cache, M, a) : launch_blocks(s, kv8_write_kernel<64, u16>, 64, *cache, M, a);
+}
+
+extern "C" int bd_k_kv8_read(void* hip_stream, const bd_kv8* cache, const int32_t* dev_from, int M, const int32_t* dev_rows, int dtype,
+                             void* dev_k_out, int64_t k_seq_stride, int64_t k_row_stride, void* dev_v_out, int64_t v_seq_stride,
+                             int64_t v_row_stride) {
+  BD_TRY(check_cache(cache, M));
+  const int64_t least = (int64_t)cache->n_kv * cache->D;
+  BD_TRY(check_rows(dev_k_out, dtype, k_seq_stride, k_row_stride, cache->n_seq, M, least));
+  BD_TRY(check_rows(dev_v_out, dtype, v_seq_stride, v_row_stride, cache->n_seq, M, least));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const Kv8ReadArgs a{*cache, {dev_from, dev_rows, M}, {dev_k_out, dev_v_out}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}};
+  if (cache->D == 128)
+    return dtype == BD_F32 ? launch_blocks(s, kv8_read_kernel<128, float>, 128, *cache, M, a) : launch_blocks(s, kv8_read_kernel<128, u16>, 128, *cache, M, a);
+  return dtype == BD_F32 ? launch_blocks(s, kv8_read_kernel<64, float>, 64, *cache, M, a) : launch_blocks(s, kv8_read_kernel<64, u16>, 64, *cache, M, a);
+}
+
+extern "C" int64_t bd_k_kv8_attention_workspace(const bd_kv8* cache, int n_q, int M, int window, int sinks) {
+  Kv8Plan p;
+  BD_TRY(check_attn(cache, n_q, M, window, sinks, true, &p));
+  return p.part_floats * 4;
+}
+
+extern "C" int bd_k_kv8_attention(void* hip_stream, const bd_kv8* cache, const void* dev_q, int64_t q_seq_stride, int64_t q_row_stride, int n_q,
+                                  int M, const int32_t* dev_rows, int mode, int window, int sinks, float scale, void* dev_out,
+                                  int64_t out_seq_stride, int64_t out_row_stride, void* dev_workspace, int64_t workspace_bytes) {
+  Kv8Plan p;
+  BD_TRY(check_attn(cache, n_q, M, window, sinks, false, &p));
+  BD_TRY(check_rows(dev_q, BD_BF16, q_seq_stride, q_row_stride, cache->n_seq, M));
+  BD_TRY(check_rows(dev_out, BD_BF16, out_seq_stride, out_row_stride, cache->n_seq, M, (int64_t)n_q * cache->D));
+  if (cache->dev_len == nullptr || (mode != BD_MODE_BIDIR && mode != BD_MODE_CAUSAL) || !(scale >= 0.f) || !std::isfinite(scale)) return BD_E_ARG;
+  if (p.part_floats > 0 && (dev_workspace == nullptr || !aligned16(dev_workspace))) return BD_E_ARG;
+  if (workspace_bytes < p.part_floats * 4) {
+    set_last_error("bd_k_kv8_attention: this shape needs %lld bytes of workspace, got %lld", (long long)p.part_floats * 4, (long long)workspace_bytes);
+    return BD_E_CAPACITY;
+  }
+  Kv8AttnArgs a{};
+  a.c = *cache;
+  a.r = {cache->dev_len, dev_rows, M};
+  a.q = static_cast<const u16*>(dev_q); a.out = static_cast<u16*>(dev_out);
+  a.q_seq = q_seq_stride; a.q_row = q_row_stride; a.o_seq = out_seq_stride; a.o_row = out_row_stride;
+  a.part = static_cast<float*>(dev_workspace);
+  a.n_q = n_q; a.mode = mode; a.window = window; a.sinks = sinks;
+  a.c_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)cache->D)) * 1.4426950408889634f;
+  a.tiles = p.tiles; a.groups = p.groups; a.chunks = p.chunks;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return cache->D == 128 ? launch_attn<128, 1>(s, a, p) : launch_attn<64, 1>(s, a, p);
+}
+
+extern "C" int bd_k_rope_plan(bd_rope* out, int D, int rotary_dim, int layout, double theta, int scaling, double factor, int trained) {
+  if (out == nullptr || (D != 64 && D != 128) || rotary_dim < 2 || rotary_dim > D || rotary_dim % 2 != 0) return BD_E_ARG;
+  if (layout != BD_ROPE_HALF && layout != BD_ROPE_INTERLEAVED) return BD_E_ARG;
+  if (scaling < BD_ROPE_PLAIN || scaling > BD_ROPE_PARTS || !(theta > 1.0) || !std::isfinite(theta)) return BD_E_ARG;
+  if (scaling != BD_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor) || trained < 1)) return BD_E_ARG;
+  if (scaling == BD_ROPE_BASE) {
+    if (rotary_dim <= 2) return BD_E_ARG;
+    theta *= std::pow(factor, (double)rotary_dim / (rotary_dim - 2));
+    if (!std::isfinite(theta)) return BD_E_ARG;
+  }
+  bd_rope p{};
+  p.D = D; p.rotary_dim = rotary_dim; p.layout = layout;
+  p.amplitude = scaling == BD_ROPE_PARTS ? (float)(1.0 + 0.1 * std::log(factor)) : 1.f;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    double f = std::pow(theta, -2.0 * i / rotary_dim);
+    if (scaling == BD_ROPE_LINEAR) f /= factor;
+    if (scaling == BD_ROPE_PARTS) {
+      double w = (trained * f / 6.283185307179586477 - 1.0) / 31.0;
+      w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
+      f = f * w + f / factor * (1.0 - w);
+    }
+    p.inv_freq[i] = f;
+  }
+  *out = p;
+  return BD_OK;
+}
+
+extern "C" int bd_k_rope(void* hip_stream, const bd_rope* plan, const void* dev_x, int64_t x_seq_stride, int64_t x_row_stride, void* dev_out,
+                         int64_t out_seq_stride, int64_t out_row_stride, int dtype, int n_heads, int n_seq, int M, const int32_t* dev_pos,
+                         const int32_t* dev_rows) {
+  if (plan == nullptr || (plan->D != 64 && plan->D != 128) || plan->rotary_dim < 2 || plan->rotary_dim > plan->D || plan->rotary_dim % 2 != 0 ||
+      (plan->layout != BD_ROPE_HALF && plan->layout != BD_ROPE_INTERLEAVED))
+    return BD_E_ARG;
+  if (n_heads < 1 || n_heads > (1 << 16) || n_seq < 1 || n_seq > 65535 || M < 1 || M > kMaxRows || dev_pos == nullptr) return BD_E_ARG;
+  BD_TRY(check_rows(dev_x, dtype, x_seq_stride, x_row_stride, n_seq, M));
+  BD_TRY(check_rows(dev_out, dtype, out_seq_stride, out_row_stride, n_seq, M, (int64_t)n_heads * plan->D));
+  RopeArgs a{};
+  a.plan = *plan;
+  a.x = dev_x; a.y = dev_out; a.x_seq = x_seq_stride; a.x_row = x_row_stride; a.y_seq = out_seq_stride; a.y_row = out_row_stride;
+  a.pos = dev_pos; a.rows = dev_rows; a.heads = n_heads; a.M = M;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (dtype == BD_F32) hipLaunchKernelGGL((rope_kernel<float>), dim3(M, n_seq), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((rope_kernel<u16>), dim3(M, n_seq), dim3(256), 0, s, a);
+  return check_launch();
+}

@@ -1,0 +1,102 @@
+// The key/value cache in 8 bits (include/bd_kernels.h): layout of a page, arithmetic of its scales, rules on rows and on what a
+// row sees, and the plan of the attention's launch, shared by host and device.
+#pragma once
+#include <cstring>
+
+#include "../../include/bd_kernels.h"
+#include "common.h"
+
+namespace bd {
+
+constexpr int kv8_e_min = -117, kv8_e_max = 119;   // 2^-9 2^-117 is the smallest normal fp32 number, 448 2^119 fits
+
+// Byte of token t (0..31), dimension d in a page's head: keys, and values (from byte 32 D on).  Sixteen bytes of lane l = 16 g + i
+// are two A-operands of the 16x16x32 product: for the keys of tile t8, row i, two k-steps; for the values rows i of two
+// d-tiles over tokens 8 g ..  The keys' rows are dealt out as in the bf16 cache (kp_index): the two tiles of scores line up with the operand of the second
+// product.  The values' rows put the eight results of a lane's tile pair on neighbouring dimensions: one 16-byte store.
+__host__ __device__ inline int kv8_k_byte(int tok, int d, int D) {
+  const int t8 = (tok >> 2) & 1, i = (tok >> 3) * 4 + (tok & 3);
+  return ((t8 * (D >> 6) + (d >> 6)) * 4 + ((d >> 4) & 3)) * 256 + i * 16 + (d & 15);
+}
+__host__ __device__ inline int kv8_v_byte(int tok, int d) {
+  return ((d >> 5) * 4 + (tok >> 3)) * 256 + (((d >> 3) & 3) * 4 + (d & 3)) * 16 + ((d >> 2) & 1) * 8 + (tok & 7);
+}
+
+// Smallest e in [kv8_e_min, kv8_e_max] with amax <= 448 2^e; bits: those of a finite amax >= 0.  (448 = 1.75 2^8)
+__host__ __device__ inline int kv8_exponent(uint32_t bits) {
+  const int x = (int)(bits >> 23) - 127;
+  const int e = (bits & 0x7FFFFFu) <= 0x600000u ? x - 8 : x - 7;
+  return e < kv8_e_min ? kv8_e_min : e > kv8_e_max ? kv8_e_max : e;
+}
+// The exponent that a scale word's byte stands for; bytes that no write leaves count as the nearest that one can.
+__host__ __device__ inline int kv8_byte_exponent(uint32_t byte) {
+  const int e = (int)(byte & 255u) - 127;
+  return e < kv8_e_min ? kv8_e_min : e > kv8_e_max ? kv8_e_max : e;
+}
+constexpr uint32_t kv8_v_nan = 1u << 16;
+
+// Rows of a sequence: `rows` of at most M at positions from `first` on, within max_blocks pages.  False: left out, and reported.
+__host__ __device__ inline bool kv8_rows_ok(int first, int rows, int M, int max_blocks) {
+  return first >= 0 && rows >= 0 && rows <= M && (int64_t)first + rows <= (int64_t)max_blocks * BD_KV8_PAGE;
+}
+
+// What rows r0 .. r1 (positions n + r0 .. n + r1) of a sequence with `rows` rows can see: the blocks of the first `sinks`
+// positions, then those from the window's start to the last visible key: block number idx of `count` is idx for
+// idx < sink_blocks, and first_block + idx - sink_blocks from there.  [clear_lo, clear_hi): blocks from the window all of whose keys every
+// row sees; clear_sinks: so many of the sink blocks too.
+struct Kv8Span { int sink_blocks, first_block, count, clear_lo, clear_hi, clear_sinks; };
+__host__ __device__ inline Kv8Span kv8_span(int n, int rows, int r0, int r1, int mode, int window, int sinks) {
+  Kv8Span s;
+  const int end = mode == BD_MODE_CAUSAL ? n + r1 + 1 : n + rows;                 // keys from here on are invisible to all
+  const int all = mode == BD_MODE_CAUSAL ? n + r0 + 1 : n + rows;                 // keys up to here are not too late for any
+  const int lo = window > 0 && n + r0 >= window ? n + r0 - window + 1 : 0;        // window of the first row, of the last
+  const int hi = window > 0 && n + r1 >= window ? n + r1 - window + 1 : 0;
+  const int snk = window > 0 ? (sinks < lo ? sinks : lo) : 0;
+  s.first_block = lo / 32;
+  s.sink_blocks = (snk + 31) / 32;
+  if (s.sink_blocks > s.first_block) s.sink_blocks = s.first_block;
+  s.count = s.sink_blocks + (end + 31) / 32 - s.first_block;
+  s.clear_lo = window > 0 && hi <= sinks ? s.first_block : (hi + 31) / 32;
+  s.clear_hi = all / 32;
+  const int early = sinks < all ? sinks : all;
+  s.clear_sinks = early / 32;
+  return s;
+}
+__host__ __device__ inline bool kv8_sees(int p, int key, int end, int mode, int window, int sinks) {
+  return key < end && (mode != BD_MODE_CAUSAL || key <= p) && (window <= 0 || p - key < window || key < sinks);
+}
+
+// Launch plan of the attention.
+struct Kv8Plan {
+  int tiles;        // tiles of 16 columns of a (sequence, kv head): column = row * G + head of the group
+  int JT, groups;   // tiles per workgroup, workgroups for a (sequence, kv head, chunk)
+  int chunks;       // workgroups that share out the blocks of a group, at most
+  int64_t part_floats;   // workspace: unnormalised partial results, [sequence][kv head][tile][chunk]
+};
+constexpr int kv8_blocks_per_chunk = 8;
+inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_blocks, int window, int sinks) {
+  Kv8Plan p{};
+  p.tiles = (int)(((int64_t)M * (n_q / n_kv) + 15) / 16);
+  p.JT = 1;
+  p.groups = ceil_div(p.tiles, p.JT);
+  int64_t blocks = max_blocks;
+  if (window > 0) {
+    const int64_t w = ((int64_t)window + M + 62) / 32 + 1 + ((int64_t)sinks + 31) / 32;
+    if (w < blocks) blocks = w;
+  }
+  const int64_t items = (int64_t)n_seq * n_kv * p.groups;
+  int64_t c = (1024 + items - 1) / items;
+  const int64_t most = (blocks + kv8_blocks_per_chunk - 1) / kv8_blocks_per_chunk;
+  if (c > most) c = most;
+  if (c > 64) c = 64;
+  p.chunks = c < 1 ? 1 : (int)c;
+  p.part_floats = p.chunks > 1 ? (int64_t)n_seq * n_kv * p.tiles * p.chunks * (16 * D + 32) : 0;
+  return p;
+}
+// Chunks that a group of `count` blocks really uses.
+__host__ __device__ inline int kv8_chunks_used(int count, int chunks) {
+  const int c = (count + kv8_blocks_per_chunk - 1) / kv8_blocks_per_chunk;
+  return c < 1 ? 1 : c < chunks ? c : chunks;
+}
+
+}  // namespace bd

@@ -1,0 +1,90 @@
+"""The 8-bit key/value cache and the rotary positions without a GPU: rules that host and device share (csrc/kv8.h) and refusals of the entry
+points under the sanitizers, the plan of the rotary positions against its formulas, and what the binding refuses."""
+import math
+import os
+import shutil
+import subprocess
+
+import pytest
+import torch
+
+from paper_2604_06832_amd import binding
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+PKG = os.path.join(ROOT, "paper_2604_06832_amd")
+BUILD = os.path.join(PKG, "_build")
+HIPCC = "/opt/rocm/bin/hipcc"
+CLANG = "/opt/rocm/lib/llvm/bin/clang++"
+OTHER_UNITS = ["bd_lib", "k_stream", "k_mega", "k_prefill", "k_attention"]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    if not os.path.exists(binding.LIB_PATH):
+        import __graft_entry__ as g
+        g.build()
+
+
+def _run(cmd):
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, " ".join(cmd) + "\n" + r.stdout[-4000:]
+    return r.stdout
+
+
+@pytest.mark.skipif(not (os.path.exists(HIPCC) and os.path.exists(CLANG)), reason="no ROCm compiler here")
+def test_shared_rules_and_refusals_under_asan_and_ubsan(tmp_path):
+    if not all(os.path.exists(os.path.join(BUILD, u + ".o")) for u in OTHER_UNITS):
+        import __graft_entry__ as g
+        g.build()
+    d = str(tmp_path)
+    _run([HIPCC, "--offload-arch=gfx950", "-O1", "-g", "-std=c++17", "-fPIC", "-Wno-unused-value", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+          "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=undefined",
+          "-c", os.path.join(PKG, "csrc", "k_kv8.hip"), "-o", os.path.join(d, "k_kv8.o")])
+    _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-shared-libsan",
+          os.path.join(d, "k_kv8.o"), *[os.path.join(BUILD, u + ".o") for u in OTHER_UNITS], "-o", os.path.join(d, "libbd_san.so")])
+    rt = os.path.dirname(_run([CLANG, "-print-file-name=libclang_rt.asan-x86_64.so"]).strip())
+    _run([HIPCC, "-x", "hip", "--offload-host-only", "-std=c++17", "-g", "-O1", "-Wno-unused-value", "-Xarch_host", "-fsanitize=address", "-Xarch_host",
+          "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=undefined", "-shared-libsan", os.path.join(ROOT, "tests", "kv8_rules_check.cpp"),
+          "-L" + d, "-lbd_san", "-Wl,-rpath," + d, "-Wl,-rpath," + rt, "-o", os.path.join(d, "check")])
+    # (what the ROCm runtime keeps until the process ends is not the library's)
+    r = subprocess.run([os.path.join(d, "check")], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300,
+                       env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0", UBSAN_OPTIONS="print_stacktrace=1"))
+    shutil.rmtree(d, ignore_errors=True)
+    assert r.returncode == 0 and "ALL OK" in r.stdout, r.stdout[-3000:]
+    assert "ERROR: AddressSanitizer" not in r.stdout and "runtime error:" not in r.stdout, r.stdout[-3000:]
+
+
+@pytest.mark.parametrize("scaling", [binding.BD_ROPE_PLAIN, binding.BD_ROPE_LINEAR, binding.BD_ROPE_BASE, binding.BD_ROPE_PARTS])
+@pytest.mark.parametrize("D,R,theta,factor,trained", [(128, 128, 1e6, 4.0, 8192), (64, 34, 1e4, 8.5, 2048), (128, 4, 5e5, 1.0, 1), (64, 64, 1e6, 32.0, 1 << 20)])
+def test_plan_of_rotary_positions(scaling, D, R, theta, factor, trained):
+    plan = binding.bd_k_rope_plan(D, R, binding.BD_ROPE_INTERLEAVED, theta, scaling, factor, trained)
+    assert (plan.D, plan.rotary_dim, plan.layout) == (D, R, binding.BD_ROPE_INTERLEAVED)
+    for i in range(R // 2):
+        f = math.exp(-2.0 * i / R * math.log(theta))
+        if scaling == binding.BD_ROPE_LINEAR:
+            f /= factor
+        elif scaling == binding.BD_ROPE_BASE:
+            f *= math.exp(-2.0 * i / (R - 2) * math.log(factor))          # (theta s^(R/(R-2)))^(-2i/R)
+        elif scaling == binding.BD_ROPE_PARTS:
+            w = min(max((trained * f / (2 * math.pi) - 1) / 31, 0.0), 1.0)
+            f = w * f + (1 - w) * f / factor
+        assert abs(plan.inv_freq[i] - f) <= 1e-14 * f * max(1.0, math.log(theta))
+    assert abs(plan.amplitude - (1 + 0.1 * math.log(factor) if scaling == binding.BD_ROPE_PARTS else 1)) <= 2.0 ** -23
+    if scaling == binding.BD_ROPE_BASE:                                    # the slowest pair is stretched by the factor, the fastest not at all
+        plain = binding.bd_k_rope_plan(D, R, 0, theta)
+        assert plan.inv_freq[0] == 1.0 and abs(plain.inv_freq[R // 2 - 1] / plan.inv_freq[R // 2 - 1] / factor - 1) < 1e-12
+
+
+def test_plan_refusals_reach_python():
+    for args in ((96, 64), (64, 65), (64, 128)):
+        with pytest.raises(binding.BdError) as e:
+            binding.bd_k_rope_plan(*args)
+        assert e.value.code == binding.BD_E_ARG
+
+
+def test_binding_takes_no_host_tensors():
+    pages, lens = torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        binding.Kv8Cache(torch.zeros((2, 1, 4096), dtype=torch.uint8), torch.zeros((2, 1), dtype=torch.int32), pages, lens)
+    with pytest.raises(ValueError):
+        binding.bd_k_rope(binding.bd_k_rope_plan(64), torch.zeros((1, 1, 1, 64)), lens)
