@@ -354,45 +354,59 @@ def bd_k_attention_static(q, k, v, n_prefix: int, mode: int, out=None):
 
 
 # -- attention on a key/value cache in 8 bits (include/bd_kernels.h) --------------------------------------------------------
+# (A step makes these calls once a layer: what the checks and the call cost on the host counts, 4 to 5 us in all with the launch.)
 
-def _rows_of(t, name, heads, D, device):
-    """(pointer, stride between sequences, stride between rows) of a tensor of rows [n_seq, M, heads, D]."""
-    if t.dim() != 4 or t.shape[2] != heads or t.shape[3] != D:
-        raise ValueError(f"{name}: expected [n_seq, M, {heads}, {D}], got {list(t.shape)}")
-    n, m, _, _ = t.shape
+_torch = None
+
+
+def _with_torch():
+    """torch, imported on first use."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _rows_of(t, name, heads, D, index):
+    """(pointer, stride between sequences, stride between rows) of a tensor of rows [n_seq, M, heads, D] on device `index`."""
+    shape = t.shape
+    if len(shape) != 4 or shape[2] != heads or shape[3] != D:
+        raise ValueError(f"{name}: expected [n_seq, M, {heads}, {D}], got {list(shape)}")
     s0, s1, s2, s3 = t.stride()
-    if s3 != 1 or (heads > 1 and s2 != D) or t.device != device:
-        raise ValueError(f"{name}: heads and dimensions have to be contiguous, on {device}")
-    return t.data_ptr(), s0 if n > 1 else 0, s1 if m > 1 else 0
+    if s3 != 1 or (s2 != D and heads > 1) or t.get_device() != index:
+        raise ValueError(f"{name}: heads and dimensions have to be contiguous, on cuda:{index}")
+    return t.data_ptr(), s0, s1
 
 
-def _ints_of(t, name, n_seq, device):
+def _ints_of(t, name, n_seq, index):
     """Pointer of an int32 tensor with one number for each sequence; None passes NULL."""
-    import torch
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.numel() != n_seq or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{name}: expected {n_seq} int32 numbers on {device}")
+    if t.dtype is not _torch.int32 or t.numel() != n_seq or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n_seq} int32 numbers on cuda:{index}")
     return t.data_ptr()
 
 
 def _dtype_of(t, name):
-    import torch
-    if t.dtype == torch.bfloat16:
+    dtype = t.dtype
+    if dtype is _torch.bfloat16:
         return BD_BF16
-    if t.dtype == torch.float32:
+    if dtype is _torch.float32:
         return BD_F32
-    raise ValueError(f"{name}: bfloat16 or float32, got {t.dtype}")
+    raise ValueError(f"{name}: bfloat16 or float32, got {dtype}")
 
 
-def _enqueue(device, call, *args):
-    """call(stream, *args) on the device's current stream."""
-    import torch
-    if torch.cuda.current_device() == device.index:
-        _check(call(torch.cuda.current_stream(device).cuda_stream, *args))
+def _enqueue(index, call, *args):
+    """call(stream, *args) on the current stream of device `index`."""
+    C_ = _torch._C
+    if C_._cuda_getDevice() == index:
+        code = call(C_._cuda_getCurrentRawStream(index), *args)
     else:
-        with torch.cuda.device(device):
-            _check(call(torch.cuda.current_stream(device).cuda_stream, *args))
+        with _torch.cuda.device(index):
+            code = call(C_._cuda_getCurrentRawStream(index), *args)
+    if code < 0:
+        raise BdError(code)
 
 
 class Kv8Cache:
@@ -402,70 +416,72 @@ class Kv8Cache:
     (positions held; moved on by the caller), status None or one int32.  The tensors are kept alive, and looked at when the kernels run."""
 
     def __init__(self, codes, scales, pages, lens, status=None):
-        import torch
+        torch = _with_torch()
         if codes.dtype != torch.uint8 or codes.dim() != 3 or not codes.is_cuda or not codes.is_contiguous():
             raise ValueError("codes: expected a contiguous uint8 tensor [n_pages, n_kv, 64 D] on the GPU")
         n_pages, n_kv, size = codes.shape
-        self.device = codes.device
-        if scales.dtype != torch.int32 or list(scales.shape) != [n_pages, n_kv] or not scales.is_contiguous() or scales.device != self.device:
-            raise ValueError(f"scales: expected a contiguous int32 tensor [{n_pages}, {n_kv}] on {self.device}")
-        if pages.dtype != torch.int32 or pages.dim() != 2 or not pages.is_contiguous() or pages.device != self.device:
-            raise ValueError(f"pages: expected a contiguous int32 tensor [n_seq, max_blocks] on {self.device}")
-        self.n_seq, self.n_kv, self.D = pages.shape[0], n_kv, size // 64
-        self._keep = (codes, scales, pages, lens, status)
-        self._c = bd_kv8(codes.data_ptr(), scales.data_ptr(), pages.data_ptr(), _ints_of(lens, "lens", self.n_seq, self.device),
-                         _ints_of(status, "status", 1, self.device), n_pages, n_kv, self.D if size % 64 == 0 else 0, self.n_seq, pages.shape[1])
+        index = codes.get_device()
+        if scales.dtype != torch.int32 or list(scales.shape) != [n_pages, n_kv] or not scales.is_contiguous() or scales.get_device() != index:
+            raise ValueError(f"scales: expected a contiguous int32 tensor [{n_pages}, {n_kv}] on cuda:{index}")
+        if pages.dtype != torch.int32 or pages.dim() != 2 or not pages.is_contiguous() or pages.get_device() != index:
+            raise ValueError(f"pages: expected a contiguous int32 tensor [n_seq, max_blocks] on cuda:{index}")
+        self.index, self.n_seq, self.n_kv, self.D = index, pages.shape[0], n_kv, size // 64
+        if lens is None:
+            raise ValueError("lens: expected one int32 for each sequence")
+        self.codes, self.scales, self.pages, self.lens, self.status = codes, scales, pages, lens, status
+        self._c = bd_kv8(codes.data_ptr(), scales.data_ptr(), pages.data_ptr(), _ints_of(lens, "lens", self.n_seq, index),
+                         _ints_of(status, "status", 1, index), n_pages, n_kv, self.D if size % 64 == 0 else 0, self.n_seq, pages.shape[1])
         self._p = C.addressof(self._c)
+        L = lib()
+        self._write, self._read, self._attention, self._workspace = (L.bd_k_kv8_write, L.bd_k_kv8_read, L.bd_k_kv8_attention,
+                                                                     L.bd_k_kv8_attention_workspace)
 
     @staticmethod
     def empty(n_pages, n_kv, D, pages, lens, status=None):
         """A cache of n_pages pages that hold nothing yet."""
-        import torch
+        torch = _with_torch()
         return Kv8Cache(torch.zeros((n_pages, n_kv, 64 * D), dtype=torch.uint8, device=pages.device),
                         torch.zeros((n_pages, n_kv), dtype=torch.int32, device=pages.device), pages, lens, status)
 
-    def _batch(self, t, name):
-        if t.shape[0] != self.n_seq:
-            raise ValueError(f"{name}: {t.shape[0]} sequences, the cache has {self.n_seq}")
-        return t.shape[1]
+    def _pair(self, k, v, what):
+        """Pointers and strides of keys and values, their type and M."""
+        index, shape = self.index, k.shape
+        kp = _rows_of(k, "keys", self.n_kv, self.D, index)
+        vp = _rows_of(v, "values", self.n_kv, self.D, index)
+        if shape[0] != self.n_seq or v.shape != shape or v.dtype is not k.dtype:
+            raise ValueError(f"{what}: keys and values have the same shape, with {self.n_seq} sequences, and type")
+        return kp, vp, _dtype_of(k, "keys"), shape[1]
 
     def bd_k_kv8_write(self, k, v, rows=None):
         """Keys and values [n_seq, M, n_kv, D] (bfloat16 or float32) to positions lens ..."""
-        kp, vp = _rows_of(k, "k", self.n_kv, self.D, self.device), _rows_of(v, "v", self.n_kv, self.D, self.device)
-        M = self._batch(k, "k")
-        if v.shape != k.shape or v.dtype != k.dtype:
-            raise ValueError("k and v: same shape and type")
-        _enqueue(self.device, lib().bd_k_kv8_write, self._p, *kp, *vp, _dtype_of(k, "k"), M, _ints_of(rows, "rows", self.n_seq, self.device))
+        kp, vp, dtype, M = self._pair(k, v, "bd_k_kv8_write")
+        _enqueue(self.index, self._write, self._p, *kp, *vp, dtype, M, _ints_of(rows, "rows", self.n_seq, self.index))
 
     def bd_k_kv8_read(self, start, k_out, v_out, rows=None):
         """Positions start .. (None: from 0) as values, to k_out and v_out [n_seq, M, n_kv, D]."""
-        kp, vp = _rows_of(k_out, "k_out", self.n_kv, self.D, self.device), _rows_of(v_out, "v_out", self.n_kv, self.D, self.device)
-        M = self._batch(k_out, "k_out")
-        if v_out.shape != k_out.shape or v_out.dtype != k_out.dtype:
-            raise ValueError("k_out and v_out: same shape and type")
-        _enqueue(self.device, lib().bd_k_kv8_read, self._p, _ints_of(start, "start", self.n_seq, self.device), M,
-                 _ints_of(rows, "rows", self.n_seq, self.device), _dtype_of(k_out, "k_out"), *kp, *vp)
+        kp, vp, dtype, M = self._pair(k_out, v_out, "bd_k_kv8_read")
+        _enqueue(self.index, self._read, self._p, _ints_of(start, "start", self.n_seq, self.index), M,
+                 _ints_of(rows, "rows", self.n_seq, self.index), dtype, *kp, *vp)
 
     def bd_k_kv8_attention_workspace(self, n_q, M, window=0, sinks=0) -> int:
-        return _check(lib().bd_k_kv8_attention_workspace(self._p, n_q, M, window, sinks))
+        return _check(self._workspace(self._p, n_q, M, window, sinks))
 
     def bd_k_kv8_attention(self, q, out, mode, window=0, sinks=0, scale=0.0, rows=None, workspace=None):
         """Attention of q [n_seq, M, n_q, D] (bfloat16) on the cache, to out (same shape).  workspace: a uint8 tensor of
         bd_k_kv8_attention_workspace bytes that nothing else uses while the call runs; None takes one from torch for this call."""
-        import torch
-        if q.dim() != 4 or q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape != q.shape:
-            raise ValueError("q and out: bfloat16 [n_seq, M, n_q, D], same shape")
-        n_q = q.shape[2]
-        qp, op = _rows_of(q, "q", n_q, self.D, self.device), _rows_of(out, "out", n_q, self.D, self.device)
-        M = self._batch(q, "q")
+        shape, index, bf16 = q.shape, self.index, _torch.bfloat16
+        if len(shape) != 4 or shape[0] != self.n_seq or q.dtype is not bf16 or out.dtype is not bf16 or out.shape != shape:
+            raise ValueError(f"q and out: bfloat16 [{self.n_seq}, M, n_q, {self.D}], same shape")
+        _, M, n_q, _ = shape
+        qp, op = _rows_of(q, "q", n_q, self.D, index), _rows_of(out, "out", n_q, self.D, index)
         if workspace is None:
-            size = self.bd_k_kv8_attention_workspace(n_q, M, window, sinks)
-            workspace = torch.empty(size, dtype=torch.uint8, device=self.device) if size else None
-        elif workspace.device != self.device or not workspace.is_contiguous():
-            raise ValueError(f"workspace: expected a contiguous tensor on {self.device}")
+            wn = self._workspace(self._p, n_q, M, window, sinks)
+            if wn > 0:
+                workspace = _torch.empty(wn, dtype=_torch.uint8, device=q.device)
+        elif workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous tensor on cuda:{index}")
         wp, wn = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
-        _enqueue(self.device, lib().bd_k_kv8_attention, self._p, *qp, n_q, M, _ints_of(rows, "rows", self.n_seq, self.device), mode, window,
-                 sinks, scale, *op, wp, wn)
+        _enqueue(index, self._attention, self._p, *qp, n_q, M, _ints_of(rows, "rows", self.n_seq, index), mode, window, sinks, scale, *op, wp, wn)
         return out
 
 
@@ -478,15 +494,17 @@ def bd_k_rope_plan(D, rotary_dim=None, layout=BD_ROPE_HALF, theta=1.0e6, scaling
 
 def bd_k_rope(plan, x, pos, out=None, rows=None):
     """The rows x [n_seq, M, heads, D] turned by their positions pos[s] + row, to out (None: a new tensor; x itself: in place)."""
-    import torch
-    if x.dim() != 4:
-        raise ValueError(f"x: expected [n_seq, M, heads, D], got {list(x.shape)}")
-    n, M, heads, _ = x.shape
+    torch = _torch or _with_torch()
+    shape, index = x.shape, x.get_device()
+    if len(shape) != 4 or index < 0:
+        raise ValueError(f"x: expected [n_seq, M, heads, D] on the GPU, got {list(shape)}")
+    n, M, heads, D = shape
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if rows is None else torch.zeros(x.shape, dtype=x.dtype, device=x.device)
-    if not x.is_cuda or out.shape != x.shape or out.dtype != x.dtype:
-        raise ValueError("x and out: same shape and type, on the GPU")
-    xp, op = _rows_of(x, "x", heads, plan.D, x.device), _rows_of(out, "out", heads, plan.D, x.device)
-    _enqueue(x.device, lib().bd_k_rope, C.addressof(plan), *xp, *op, _dtype_of(x, "x"), heads, n, M, _ints_of(pos, "pos", n, x.device),
-             _ints_of(rows, "rows", n, x.device))
+        out = torch.empty(shape, dtype=x.dtype, device=x.device) if rows is None else torch.zeros(shape, dtype=x.dtype, device=x.device)
+    elif out.shape != shape or out.dtype is not x.dtype:
+        raise ValueError("x and out: same shape and type")
+    if D != plan.D:
+        raise ValueError(f"x: heads of {D}, the plan is for {plan.D}")
+    _enqueue(index, lib().bd_k_rope, C.addressof(plan), *_rows_of(x, "x", heads, D, index), *_rows_of(out, "out", heads, D, index), _dtype_of(x, "x"),
+             heads, n, M, _ints_of(pos, "pos", n, index), _ints_of(rows, "rows", n, index))
     return out

@@ -1,4 +1,5 @@
 // Attention on a key/value cache in 8 bits, and what fills and reads it (include/bd_kernels.h: bd_rope, bd_kv8).
+#include <atomic>
 #include <cmath>
 
 #include "kv8.h"
@@ -250,26 +251,30 @@ struct Kv8AttnArgs {
   float* part;
   int n_q, mode, window, sinks;
   float c_log2;                 // scale * log2(e)
-  int tiles, groups, chunks;
+  int tiles, groups, chunks, runs, run_len;
 };
 constexpr float kv8_lowest = -3.0e38f;   // start of a running maximum: below every finite score, and finite itself
 
-// A block's codes, as the lanes load them, and its scale word.
+// A block's codes, as the lanes load them.
 template <int D>
 struct Kv8Block {
   uint4 k[2][D / 64], v[D / 32];
-  uint32_t word;
 };
 template <int D>
-__device__ inline void kv8_load(Kv8Block<D>& b, const bd_kv8& c, int page, int h, uint32_t word, int lane) {
-  const uint4* p = reinterpret_cast<const uint4*>(c.dev_codes + ((size_t)page * c.n_kv + h) * (64 * D)) + lane;
+__device__ inline const uint4* kv8_codes(const bd_kv8& c, int page, int h, int lane) {
+  return reinterpret_cast<const uint4*>(c.dev_codes + ((size_t)page * c.n_kv + h) * (64 * D)) + lane;
+}
+template <int D>
+__device__ inline void kv8_load_k(Kv8Block<D>& b, const uint4* p) {
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) b.k[t][j] = p[(t * (D / 64) + j) * 64];
+}
+template <int D>
+__device__ inline void kv8_load_v(Kv8Block<D>& b, const uint4* p) {
 #pragma unroll
   for (int j = 0; j < D / 32; ++j) b.v[j] = p[(D / 32 + j) * 64];
-  b.word = word;
 }
 // Eight codes times 2^e as a bf16 operand (exact).
 __device__ inline bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
@@ -280,14 +285,32 @@ __device__ inline bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
   o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return o.v;
 }
+// High bit of each byte that holds a NaN.
+__device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+__device__ inline uint32_t without_nan(uint32_t w) { return w & ~((nan_bytes(w) >> 7) * 255u); }
 
-// One block of 32 keys against JT tiles of 16 columns.  S^T = K Q^T, so that a lane has eight scores of one column, and
-// O^T = V^T P^T.  The running maximum follows the scores only when one exceeds it by more than 2^8: weights up to 256 lose nothing.
-template <int D, int JT, bool MASKED>
-__device__ inline void kv8_block(const Kv8Block<D>& b, const bf16x8 (&qf)[JT][D / 32], f32x4 (&O)[JT][D / 16], float (&mrun)[JT], float (&lrun)[JT],
-                                 int kb, const int (&p)[JT], int end, const Kv8AttnArgs& a, int g, float c) {
+// What a wavefront knows of the rows it works for.
+template <int JT>
+struct Kv8Cols {
+  int p[JT];                    // position of its column's row in each tile
+  int end;                      // keys from here on are invisible
+};
+template <int JT>
+__device__ inline bool kv8_visible(const Kv8Cols<JT>& w, const Kv8AttnArgs& a, int jt, int key) {
+  return kv8_sees(w.p[jt], key, w.end, a.mode, a.window, a.sinks);
+}
+
+// One block of 32 keys against JT tiles of 16 columns.  S^T = K Q^T, so that a lane has eight scores of one column, and O^T = V^T P^T.
+// The running maximum follows the scores only when one exceeds it by more than 2^8: weights up to 256 lose nothing, and most
+// blocks need no maximum across lanes.  The sum of the weights is a product too, with a row of ones: what divides the result are the
+// same rounded weights that make it.  Once a block's keys are in operands the next block's are loaded over them, then likewise the values: each
+// load has the other half of a block to arrive.
+template <int D, int JT>
+__device__ inline void kv8_block(Kv8Block<D>& b, uint32_t word, bool clear, const uint4* next, const bf16x8 (&qf)[JT][D / 32], f32x4 (&O)[JT][D / 16], float (&mrun)[JT],
+                                 f32x4 (&L)[JT], int kb, const Kv8Cols<JT>& cols, const Kv8AttnArgs& a, int g) {
   constexpr int DT = D / 16;
-  const float ks = two_to(kv8_byte_exponent(b.word)), vs = two_to(kv8_byte_exponent(b.word >> 8));
+  const float c = a.c_log2;
+  const float ks = two_to(kv8_byte_exponent(word)), vs = two_to(kv8_byte_exponent(word >> 8));
   f32x4 s[JT][2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
@@ -302,27 +325,35 @@ __device__ inline void kv8_block(const Kv8Block<D>& b, const bf16x8 (&qf)[JT][D 
       for (int jt = 0; jt < JT; ++jt) s[jt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[jt][2 * j + 1], s[jt][t], 0, 0, 0);
     }
   }
-  float cm[JT];
+  __builtin_amdgcn_sched_barrier(0);                    // (the loads stay behind the last use of what they overwrite)
+  kv8_load_k<D>(b, next);
+  if (!clear) {
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[jt][e >> 2][e & 3] = kv8_visible<JT>(cols, a, jt, kb * 32 + 8 * g + e) ? s[jt][e >> 2][e & 3] : -INFINITY;
+    if ((word & kv8_v_nan) != 0u) {
+      // 0 times a NaN would reach rows that do not see it: kv8_nan_rows puts it where it belongs
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) b.v[j] = make_uint4(without_nan(b.v[j].x), without_nan(b.v[j].y), without_nan(b.v[j].z), without_nan(b.v[j].w));
+    }
+  }
+  float m[JT];
   bool move = false;
 #pragma unroll
   for (int jt = 0; jt < JT; ++jt) {
-    float m = -INFINITY;
+    m[jt] = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (MASKED)
-        if (!kv8_sees(p[jt], kb * 32 + 8 * g + e, end, a.mode, a.window, a.sinks)) s[jt][e >> 2][e & 3] = -INFINITY;
-      m = fmaxf(m, s[jt][e >> 2][e & 3]);
-    }
-    cm[jt] = rows_max(m) * c;
-    move |= cm[jt] > mrun[jt] + 8.f;
+    for (int e = 0; e < 8; ++e) m[jt] = fmaxf(m[jt], s[jt][e >> 2][e & 3]);
+    move |= m[jt] * c > mrun[jt] + 8.f;
   }
   if (__builtin_amdgcn_ballot_w64(move) != 0ull) {
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt) {
-      const float mnew = fmaxf(mrun[jt], cm[jt]);
+      const float mnew = fmaxf(mrun[jt], rows_max(m[jt]) * c);
       const float alpha = __builtin_amdgcn_exp2f(mrun[jt] - mnew);
       mrun[jt] = mnew;
-      lrun[jt] *= alpha;
+      L[jt] *= alpha;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) O[jt][dt] *= alpha;
     }
@@ -331,38 +362,13 @@ __device__ inline void kv8_block(const Kv8Block<D>& b, const bf16x8 (&qf)[JT][D 
 #pragma unroll
   for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float w = __builtin_amdgcn_exp2f(fmaf(s[jt][e >> 2][e & 3], c, -mrun[jt]));      // (an invisible key's is 0)
-      lrun[jt] += w;
-      p8[jt][e] = (__bf16)w;      // rounded for the product: at most 2^-9 of a weight, independent from key to key
-    }
-  if (MASKED && (b.word & kv8_v_nan) != 0u) {
-    // A NaN among the values of a block that not every row sees all of: 0 times it would be NaN in rows that do not see it.  The product
-    // runs without them, and a second one counts for each row and dimension the visible NaN.
+    for (int e = 0; e < 8; ++e)         // (rounded for the product: by at most 2^-8 of a weight, independently from key to key; an invisible key's is 0)
+      p8[jt][e] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[jt][e >> 2][e & 3], c, -mrun[jt]));
+  bf16x8 one;
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
+  for (int e = 0; e < 8; ++e) one[e] = (__bf16)1.f;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        bf16x8 v = widen8(u ? b.v[j].z : b.v[j].x, u ? b.v[j].w : b.v[j].y, vs), one;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool bad = (float)v[e] != (float)v[e];
-          one[e] = bad ? (__bf16)1.f : (__bf16)0.f;
-          v[e] = bad ? (__bf16)0.f : v[e];
-        }
-#pragma unroll
-        for (int jt = 0; jt < JT; ++jt) {
-          bf16x8 seen;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) seen[e] = kv8_sees(p[jt], kb * 32 + 8 * g + e, end, a.mode, a.window, a.sinks) ? (__bf16)1.f : (__bf16)0.f;
-          const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-          O[jt][2 * j + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p8[jt], O[jt][2 * j + u], 0, 0, 0);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) O[jt][2 * j + u][r] = count[r] > 0.f ? NAN : O[jt][2 * j + u][r];
-        }
-      }
-    return;
-  }
+  for (int jt = 0; jt < JT; ++jt) L[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, p8[jt], L[jt], 0, 0, 0);
 #pragma unroll
   for (int j = 0; j < D / 32; ++j) {
     const bf16x8 v0 = widen8(b.v[j].x, b.v[j].y, vs), v1 = widen8(b.v[j].z, b.v[j].w, vs);
@@ -370,6 +376,33 @@ __device__ inline void kv8_block(const Kv8Block<D>& b, const bf16x8 (&qf)[JT][D 
     for (int jt = 0; jt < JT; ++jt) O[jt][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p8[jt], O[jt][2 * j], 0, 0, 0);
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt) O[jt][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p8[jt], O[jt][2 * j + 1], 0, 0, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  kv8_load_v<D>(b, next);
+}
+
+// A block with NaN among its values that not every row sees all of: results become NaN where a row sees one of its dimension.
+template <int D, int JT>
+__device__ inline void kv8_nan_rows(const uint4* codes, f32x4 (&O)[JT][D / 16], int kb, const Kv8Cols<JT>& cols, const Kv8AttnArgs& a, int g) {
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j) {
+    const uint4 v = codes[(D / 32 + j) * 64];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t n0 = nan_bytes(u ? v.z : v.x), n1 = nan_bytes(u ? v.w : v.y);
+      bf16x8 bad;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bad[e] = ((e < 4 ? n0 : n1) >> (8 * (e & 3) + 7) & 1u) != 0u ? (__bf16)1.f : (__bf16)0.f;
+#pragma unroll
+      for (int jt = 0; jt < JT; ++jt) {
+        bf16x8 seen;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) seen[e] = kv8_visible<JT>(cols, a, jt, kb * 32 + 8 * g + e) ? (__bf16)1.f : (__bf16)0.f;
+        const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) O[jt][2 * j + u][r] = count[r] > 0.f ? NAN : O[jt][2 * j + u][r];
+      }
+    }
   }
 }
 
@@ -381,38 +414,61 @@ __device__ inline void kv8_store(u16* o, const f32x4& a, const f32x4& b, float i
   *reinterpret_cast<uint4*>(o) = w.u;
 }
 
-// A workgroup of four wavefronts takes JT tiles of a (sequence, kv head) and one of the chunks of their blocks: block number idx belongs to
-// chunk idx % chunks and in it to wavefront (idx / chunks) % 4.  The wavefronts merge through LDS; a group in one chunk stores its result, of several each
-// leaves an unnormalised partial, which kv8_merge_kernel sums in the order of the chunks.  The workgroups of the tiles of one chunk have
-// numbers that differ by multiples of 8: one XCD, whose L2 then serves all but the first.
-template <int D, int JT> constexpr int kv8_attn_lds() { return 4 * JT * ((D / 16) * 1024 + 2 * 64); }
-template <int D, int JT>
-__global__ __launch_bounds__(256, JT > 2 ? 1 : 2) void kv8_attn_kernel(Kv8AttnArgs a) {
-  constexpr int DT = D / 16, NW = 4;
+// A workgroup of NW wavefronts takes JT tiles of a (sequence, kv head) and one of the chunks of their blocks: block number idx belongs to
+// chunk idx % chunks and in it to wavefront (idx / chunks) % NW.  The wavefronts merge through LDS; a group in one chunk stores its result, of several each
+// leaves an unnormalised partial, which kv8_merge_kernel sums in the order of the chunks.  The groups of a (sequence, kv head, chunk), which
+// read the same blocks, go to one XCD (numbers that differ by multiples of 8), where its L2 serves all but the first, or are dealt to several
+// where there are fewer than 8 such units; the last groups, which see most, start first.
+template <int D, int JT, int NW> constexpr int kv8_attn_lds() { return NW * JT * ((D / 16) * 1024 + 2 * 64); }
+template <int D, int JT, int NW, int AHEAD>
+__global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
+  constexpr int DT = D / 16;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   f32x4* sO = reinterpret_cast<f32x4*>(lds);                            // [NW][JT][DT][64]
   float* sm = reinterpret_cast<float*>(lds + NW * JT * DT * 1024);      // [NW][JT][16]
   float* sl = sm + NW * JT * 16;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  const int unit = (blockIdx.x / (8 * a.groups)) * 8 + (blockIdx.x & 7), grp = (blockIdx.x >> 3) % a.groups;
-  if (unit >= a.c.n_seq * a.c.n_kv * a.chunks) return;
+  const int run = (blockIdx.x / (8 * a.run_len)) * 8 + (blockIdx.x & 7), unit = run / a.runs;
+  const int grp = a.groups - 1 - ((int)(blockIdx.x >> 3) % a.run_len * a.runs + run % a.runs);
+  if (grp < 0 || unit >= a.c.n_seq * a.c.n_kv * a.chunks) return;
   const int chunk = unit % a.chunks, h = (unit / a.chunks) % a.c.n_kv, s = unit / (a.chunks * a.c.n_kv);
   int n, rows;
   if (!kv8_take(a.c, a.r, s, n, rows)) return;
-  const int G = a.n_q / a.c.n_kv, cols = rows * G, c0 = grp * JT * 16;
-  if (c0 >= cols) return;
-  const int r0 = c0 / G, r1 = (min(c0 + JT * 16, cols) - 1) / G;
+  const int G = a.n_q / a.c.n_kv, ncols = rows * G, c0 = grp * JT * 16;
+  if (c0 >= ncols) return;
+  const int r0 = c0 / G, r1 = (min(c0 + JT * 16, ncols) - 1) / G;
   const Kv8Span sp = kv8_span(n, rows, r0, r1, a.mode, a.window, a.sinks);
   const int used = kv8_chunks_used(sp.count, a.chunks);
   if (chunk >= used) return;
+  const int step = NW * used, first = wave * used + chunk;
+  const int cnt = __builtin_amdgcn_readfirstlane(sp.count > first ? (sp.count - first + step - 1) / step : 0);
+  // pages and scales of the wavefront's next 64 blocks, one a lane; a block whose page lies outside the pool counts as one past the end
+  int my_page = 0, my_kb = 0;
+  uint32_t my_word = 0;
+  auto look_up = [&](int base) {
+    my_page = 0;
+    my_word = kv8_v_nan | 0x7F7F;
+    my_kb = 1 << 25;
+    if (base + lane < cnt) {
+      const int idx = first + (base + lane) * step, kb = idx < sp.sink_blocks ? idx : sp.first_block + idx - sp.sink_blocks;
+      const int page = kv8_page(a.c, s, kb);
+      if (page >= 0) {
+        my_page = page;
+        my_kb = kb;
+        my_word = a.c.dev_scales[(size_t)page * a.c.n_kv + h];
+      }
+    }
+  };
+  look_up(0);
   bf16x8 qf[JT][D / 32];
-  f32x4 O[JT][DT];
-  float mrun[JT], lrun[JT];
-  int p[JT];
+  f32x4 O[JT][DT], L[JT];
+  float mrun[JT];
+  Kv8Cols<JT> cols;
+  cols.end = n + rows;
 #pragma unroll
   for (int jt = 0; jt < JT; ++jt) {
-    const int cc = min(c0 + jt * 16 + col, cols - 1);                   // (columns past the last one repeat it and store nothing)
-    p[jt] = n + cc / G;
+    const int cc = min(c0 + jt * 16 + col, ncols - 1);                   // (columns past the last one repeat it and store nothing)
+    cols.p[jt] = n + cc / G;
     const u16* qp = a.q + s * a.q_seq + (cc / G) * a.q_row + (h * G + cc % G) * D + 16 * g;
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
@@ -421,46 +477,61 @@ __global__ __launch_bounds__(256, JT > 2 ? 1 : 2) void kv8_attn_kernel(Kv8AttnAr
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) O[jt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    L[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
     mrun[jt] = kv8_lowest;
-    lrun[jt] = 0.f;
   }
-  const int step = NW * used, first = wave * used + chunk;
-  const int cnt = sp.count > first ? (sp.count - first + step - 1) / step : 0;
-  for (int base = 0; base < cnt; base += 64) {
-    // pages and scales of the next 64 blocks, one a lane
-    int my_page = -1;
-    uint32_t my_word = 0;
-    if (base + lane < cnt) {
-      const int idx = first + (base + lane) * step;
-      my_page = kv8_page(a.c, s, idx < sp.sink_blocks ? idx : sp.first_block + idx - sp.sink_blocks);
-      if (my_page >= 0) my_word = a.c.dev_scales[(size_t)my_page * a.c.n_kv + h];
+  // AHEAD blocks are in flight, their numbers and scales with them
+  Kv8Block<D> blk[AHEAD];
+  int kbs[AHEAD];
+  uint32_t words[AHEAD];
+  auto next_of = [&](int i, int& kb, uint32_t& word) {     // (behind the last block: some page of the pool, never used)
+    if ((i & 63) == 0 && i > 0) look_up(i);
+    kb = __builtin_amdgcn_readlane(my_kb, i & 63);
+    word = (uint32_t)__builtin_amdgcn_readlane((int)my_word, i & 63);
+    return kv8_codes<D>(a.c, __builtin_amdgcn_readlane(my_page, i & 63), h, lane);
+  };
+  auto is_clear = [&](int kb) { return kb < sp.first_block ? kb < sp.clear_sinks : kb >= sp.clear_lo && kb < sp.clear_hi; };
+  bool nan = false;
+  if (cnt > 0) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const uint4* codes = next_of(u, kbs[u], words[u]);
+      kv8_load_k<D>(blk[u], codes);
+      kv8_load_v<D>(blk[u], codes);
     }
-    const int todo = min(cnt - base, 64);
-    for (int i = 0; i < todo; ++i) {
-      const int page = __builtin_amdgcn_readlane(my_page, i);
-      if (page < 0) continue;
-      const int idx = first + (base + i) * step;
-      const bool sink = idx < sp.sink_blocks;
-      const int kb = sink ? idx : sp.first_block + idx - sp.sink_blocks;
-      Kv8Block<D> b;
-      kv8_load<D>(b, a.c, page, h, (uint32_t)__builtin_amdgcn_readlane((int)my_word, i), lane);
-      const bool clear = sink ? kb < sp.clear_sinks : kb >= sp.clear_lo && kb < sp.clear_hi;
-      if (clear) kv8_block<D, JT, false>(b, qf, O, mrun, lrun, kb, p, n + rows, a, g, a.c_log2);
-      else kv8_block<D, JT, true>(b, qf, O, mrun, lrun, kb, p, n + rows, a, g, a.c_log2);
+    for (int i = 0; i < cnt; i += AHEAD) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        if (u > 0 && i + u >= cnt) break;
+        const int kb = kbs[u];
+        const uint32_t word = words[u];
+        const bool clear = is_clear(kb);
+        const uint4* next = next_of(i + u + AHEAD, kbs[u], words[u]);
+        kv8_block<D, JT>(blk[u], word, clear, next, qf, O, mrun, L, kb, cols, a, g);
+        nan |= !clear && (word & kv8_v_nan) != 0u;
+      }
+    }
+  }
+  if (nan) {
+    for (int i = 0; i < cnt; ++i) {
+      if (i == 0) look_up(0);
+      int kb;
+      uint32_t word;
+      const uint4* codes = next_of(i, kb, word);
+      if (!is_clear(kb) && (word & kv8_v_nan) != 0u) kv8_nan_rows<D, JT>(codes, O, kb, cols, a, g);
     }
   }
 #pragma unroll
   for (int jt = 0; jt < JT; ++jt) {
-    const float l = rows_sum(lrun[jt]);
     if (g == 0) {
       sm[(wave * JT + jt) * 16 + col] = mrun[jt];
-      sl[(wave * JT + jt) * 16 + col] = l;
+      sl[(wave * JT + jt) * 16 + col] = L[jt][0];
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) sO[((wave * JT + jt) * DT + dt) * 64 + lane] = O[jt][dt];
   }
   __syncthreads();
-  // wavefront w sums pairs of d-tiles w, w + 4, ..
+  // the wavefronts share out the pairs of d-tiles
   for (int item = wave; item < JT * (DT / 2); item += NW) {
     const int jt = item / (DT / 2), j = item % (DT / 2), cc = c0 + jt * 16 + col;
     float m = kv8_lowest, f[NW], l = 0.f;
@@ -475,8 +546,8 @@ __global__ __launch_bounds__(256, JT > 2 ? 1 : 2) void kv8_attn_kernel(Kv8AttnAr
       o1 += sO[((w * JT + jt) * DT + 2 * j + 1) * 64 + lane] * f[w];
     }
     if (used == 1) {
-      if (cc < cols) kv8_store(a.out + s * a.o_seq + (cc / G) * a.o_row + (h * G + cc % G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
-    } else if (c0 + jt * 16 < cols) {
+      if (cc < ncols) kv8_store(a.out + s * a.o_seq + (cc / G) * a.o_row + (h * G + cc % G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
+    } else if (c0 + jt * 16 < ncols) {
       float* pp = a.part + ((((int64_t)s * a.c.n_kv + h) * a.tiles + grp * JT + jt) * a.chunks + chunk) * (16 * D + 32);
       *reinterpret_cast<f32x4*>(pp + (2 * j * 64 + lane) * 4) = o0;
       *reinterpret_cast<f32x4*>(pp + ((2 * j + 1) * 64 + lane) * 4) = o1;
@@ -496,16 +567,18 @@ __global__ __launch_bounds__(64) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
   const int h = sh % a.c.n_kv, s = sh / a.c.n_kv;
   int n, rows;
   if (!kv8_take(a.c, a.r, s, n, rows)) return;
-  const int G = a.n_q / a.c.n_kv, cols = rows * G, c0 = tile / JT * JT * 16, cc = tile * 16 + col;
-  if (tile * 16 >= cols) return;
-  const Kv8Span sp = kv8_span(n, rows, c0 / G, (min(c0 + JT * 16, cols) - 1) / G, a.mode, a.window, a.sinks);
+  const int G = a.n_q / a.c.n_kv, ncols = rows * G, c0 = tile / JT * JT * 16, cc = tile * 16 + col;
+  if (tile * 16 >= ncols) return;
+  const Kv8Span sp = kv8_span(n, rows, c0 / G, (min(c0 + JT * 16, ncols) - 1) / G, a.mode, a.window, a.sinks);
   const int used = kv8_chunks_used(sp.count, a.chunks);
   if (used == 1) return;
   const float* base = a.part + ((int64_t)sh * a.tiles + tile) * a.chunks * (16 * D + 32);
   float m = kv8_lowest;
+#pragma unroll 8
   for (int c = 0; c < used; ++c) m = fmaxf(m, base[c * (16 * D + 32) + 16 * D + col]);
   float l = 0.f;
   f32x4 o0 = f32x4{0.f, 0.f, 0.f, 0.f}, o1 = o0;
+#pragma unroll 4
   for (int c = 0; c < used; ++c) {
     const float* pp = base + c * (16 * D + 32);
     const float f = __builtin_amdgcn_exp2f(pp[16 * D + col] - m);
@@ -513,7 +586,7 @@ __global__ __launch_bounds__(64) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
     o0 += *reinterpret_cast<const f32x4*>(pp + (2 * j * 64 + lane) * 4) * f;
     o1 += *reinterpret_cast<const f32x4*>(pp + ((2 * j + 1) * 64 + lane) * 4) * f;
   }
-  if (cc < cols) kv8_store(a.out + s * a.o_seq + (cc / G) * a.o_row + (h * G + cc % G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
+  if (cc < ncols) kv8_store(a.out + s * a.o_seq + (cc / G) * a.o_row + (h * G + cc % G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
 }
 
 // ---- rotary positions -----------------------------------------------------------------------------------------------------
@@ -595,13 +668,22 @@ int launch_blocks(hipStream_t s, K kernel, int D, const bd_kv8& c, int M, const 
   return check_launch();
 }
 
-template <int D, int JT>
+template <int D, int JT, int NW, int AHEAD>
 int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
-  constexpr int lds = kv8_attn_lds<D, JT>();
-  if (lds > 65536) HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attn_kernel<D, JT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-  const int64_t units = (int64_t)a.c.n_seq * a.c.n_kv * p.chunks, grid = (units + 7) / 8 * 8 * p.groups;
-  if (grid >= (1 << 24)) return BD_E_ARG;               // (2^32 threads are one too many for a launch)
-  hipLaunchKernelGGL((kv8_attn_kernel<D, JT>), dim3((unsigned)grid), dim3(256), lds, s, a);
+  constexpr int lds = kv8_attn_lds<D, JT, NW>();
+  if (lds > 65536) {
+    static std::atomic<uint64_t> allowed{0};              // devices on which this kernel may have so much LDS already
+    int dev = 0;
+    HIP_TRY(hipGetDevice(&dev));
+    const uint64_t bit = (uint64_t)1 << (dev & 63);
+    if (dev > 63 || (allowed.load(std::memory_order_relaxed) & bit) == 0) {
+      HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attn_kernel<D, JT, NW, AHEAD>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+      if (dev <= 63) allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  const int64_t units = (int64_t)a.c.n_seq * a.c.n_kv * p.chunks, grid = (units * p.runs + 7) / 8 * 8 * p.run_len;
+  if (grid * NW * 64 >= ((int64_t)1 << 32)) return BD_E_ARG;
+  hipLaunchKernelGGL((kv8_attn_kernel<D, JT, NW, AHEAD>), dim3((unsigned)grid), dim3(NW * 64), lds, s, a);
   BD_TRY(check_launch());
   if (p.chunks > 1) {
     hipLaunchKernelGGL((kv8_merge_kernel<D>), dim3((unsigned)((int64_t)a.c.n_seq * a.c.n_kv * p.tiles * (D / 32))), dim3(64), 0, s, a, JT);
@@ -609,7 +691,6 @@ int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
   }
   return BD_OK;
 }
-
 int check_attn(const bd_kv8* c, int n_q, int M, int window, int sinks, bool shape_only, Kv8Plan* p) {
   BD_TRY(check_cache(c, M, shape_only));
   if (n_q < 1 || n_q > (1 << 16) || n_q % c->n_kv != 0 || window < 0 || sinks < 0) return BD_E_ARG;
@@ -676,9 +757,10 @@ extern "C" int bd_k_kv8_attention(void* hip_stream, const bd_kv8* cache, const v
   a.part = static_cast<float*>(dev_workspace);
   a.n_q = n_q; a.mode = mode; a.window = window; a.sinks = sinks;
   a.c_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)cache->D)) * 1.4426950408889634f;
-  a.tiles = p.tiles; a.groups = p.groups; a.chunks = p.chunks;
+  a.tiles = p.tiles; a.groups = p.groups; a.chunks = p.chunks; a.runs = p.runs; a.run_len = p.run_len;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  return cache->D == 128 ? launch_attn<128, 1>(s, a, p) : launch_attn<64, 1>(s, a, p);
+  if (cache->D == 128) return p.JT == 2 ? launch_attn<128, 2, 4, 2>(s, a, p) : launch_attn<128, 1, 8, 1>(s, a, p);
+  return p.JT == 2 ? launch_attn<64, 2, 4, 2>(s, a, p) : launch_attn<64, 1, 8, 1>(s, a, p);
 }
 
 extern "C" int bd_k_rope_plan(bd_rope* out, int D, int rotary_dim, int layout, double theta, int scaling, double factor, int trained) {

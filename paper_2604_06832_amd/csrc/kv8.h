@@ -1,8 +1,6 @@
 // The key/value cache in 8 bits (include/bd_kernels.h): layout of a page, arithmetic of its scales, rules on rows and on what a
 // row sees, and the plan of the attention's launch, shared by host and device.
 #pragma once
-#include <cstring>
-
 #include "../../include/bd_kernels.h"
 #include "common.h"
 
@@ -66,36 +64,48 @@ __host__ __device__ inline bool kv8_sees(int p, int key, int end, int mode, int 
   return key < end && (mode != BD_MODE_CAUSAL || key <= p) && (window <= 0 || p - key < window || key < sinks);
 }
 
-// Launch plan of the attention.
+// Launch plan of the attention.  An item is a tile of 16 columns (column = row * G + head of the group) of a (sequence, kv head).
 struct Kv8Plan {
-  int tiles;        // tiles of 16 columns of a (sequence, kv head): column = row * G + head of the group
-  int JT, groups;   // tiles per workgroup, workgroups for a (sequence, kv head, chunk)
+  int tiles;        // of a (sequence, kv head)
+  int JT, NW;       // tiles and wavefronts of a workgroup
+  int groups;       // workgroups for a unit: (sequence, kv head, chunk)
   int chunks;       // workgroups that share out the blocks of a group, at most
+  int runs, run_len;     // parts of a unit's groups that go to an XCD each, and their length
   int64_t part_floats;   // workspace: unnormalised partial results, [sequence][kv head][tile][chunk]
 };
-constexpr int kv8_blocks_per_chunk = 8;
+constexpr int kv8_chunk_blocks = 32, kv8_cus = 256;
 inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_blocks, int window, int sinks) {
   Kv8Plan p{};
   p.tiles = (int)(((int64_t)M * (n_q / n_kv) + 15) / 16);
-  p.JT = 1;
+  const int64_t items = (int64_t)n_seq * n_kv * p.tiles;
+  // More items than CUs: two tiles share each block that a wavefront loads and widens, four wavefronts, two workgroups a CU.  Else one tile and
+  // eight wavefronts, for the shortest walk.  us, (1 tile, 8) and (2 tiles, 4): 256 items behind 2048 keys 13.2 and 18.1, 512 items 25.0 and
+  // 19.8, 1024 rows (1024 items) behind 7168 keys 128 and 73.
+  const bool wide = items > kv8_cus && p.tiles > 1;
+  p.JT = wide ? 2 : 1;
+  p.NW = wide ? 4 : 8;
   p.groups = ceil_div(p.tiles, p.JT);
+  // Fewer items than CUs: the blocks of an item in chunks of about 32, four a wavefront, as far as there are CUs for them.  us, 1 / 2 / 4 / 8 /
+  // 16 chunks: one row behind 8192 keys 30 / 21 / 15 / 11.9 / 11.7, behind 1024 8.5 / 10.3 / ..; 256 items behind 2048 keys 12.2 / 18.0 / ..
   int64_t blocks = max_blocks;
   if (window > 0) {
     const int64_t w = ((int64_t)window + M + 62) / 32 + 1 + ((int64_t)sinks + 31) / 32;
     if (w < blocks) blocks = w;
   }
-  const int64_t items = (int64_t)n_seq * n_kv * p.groups;
-  int64_t c = (1024 + items - 1) / items;
-  const int64_t most = (blocks + kv8_blocks_per_chunk - 1) / kv8_blocks_per_chunk;
-  if (c > most) c = most;
+  int64_t c = (blocks + kv8_chunk_blocks / 2) / kv8_chunk_blocks;
+  if (c > kv8_cus / items) c = kv8_cus / items;
   if (c > 64) c = 64;
   p.chunks = c < 1 ? 1 : (int)c;
-  p.part_floats = p.chunks > 1 ? (int64_t)n_seq * n_kv * p.tiles * p.chunks * (16 * D + 32) : 0;
+  p.part_floats = p.chunks > 1 ? items * p.chunks * (16 * D + 32) : 0;
+  const int64_t units = (int64_t)n_seq * n_kv * p.chunks;
+  p.runs = units >= 8 ? 1 : (int)((8 + units - 1) / units);
+  if (p.runs > p.groups) p.runs = p.groups;
+  p.run_len = ceil_div(p.groups, p.runs);
   return p;
 }
 // Chunks that a group of `count` blocks really uses.
 __host__ __device__ inline int kv8_chunks_used(int count, int chunks) {
-  const int c = (count + kv8_blocks_per_chunk - 1) / kv8_blocks_per_chunk;
+  const int c = (count + kv8_chunk_blocks / 2) / kv8_chunk_blocks;
   return c < 1 ? 1 : c < chunks ? c : chunks;
 }
 

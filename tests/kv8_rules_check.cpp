@@ -93,6 +93,17 @@ static void plan() {
     const Kv8Plan p = kv8_plan(n_seq, M, n_kv * G, n_kv, D, blocks, window, 4);
     CHECK(p.tiles * 16 >= M * G && (p.tiles - 1) * 16 < M * G && p.JT >= 1 && p.groups * p.JT >= p.tiles && (p.groups - 1) * p.JT < p.tiles);
     CHECK(p.chunks >= 1 && p.chunks <= 64);
+    CHECK(p.runs >= 1 && p.runs * p.run_len >= p.groups && (p.runs == 1 || (int64_t)n_seq * n_kv * p.chunks < 8));
+    // what the kernel makes of its number: every (unit, group) once
+    const int64_t units = (int64_t)n_seq * n_kv * p.chunks, grid = (units * p.runs + 7) / 8 * 8 * p.run_len;
+    if (grid < 20000 && it < 2000) {
+      std::vector<int> seen(units * p.groups, 0);
+      for (int64_t b = 0; b < grid; ++b) {
+        const int64_t run = (b / (8 * p.run_len)) * 8 + (b & 7), unit = run / p.runs, grp = p.groups - 1 - ((b >> 3) % p.run_len * p.runs + run % p.runs);
+        if (grp >= 0 && unit < units) ++seen[unit * p.groups + grp];
+      }
+      for (int n : seen) CHECK(n == 1);
+    }
     CHECK(p.chunks > 1 ? p.part_floats == (int64_t)n_seq * n_kv * p.tiles * p.chunks * (16 * D + 32) : p.part_floats == 0);
     for (int c : {0, 1, 7, 8, 9, 100, 3000}) CHECK(kv8_chunks_used(c, p.chunks) >= 1 && kv8_chunks_used(c, p.chunks) <= p.chunks);
   }

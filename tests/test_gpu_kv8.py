@@ -264,7 +264,7 @@ def test_pages_past_32_bits_of_bytes():
     np.testing.assert_array_equal(k[0].double().cpu().numpy(), plain.v[0, :80])
     np.testing.assert_array_equal(v[0].double().cpu().numpy(), plain.v[1, :80])
     q = torch.randn((1, 1, 4, D), device="cuda").to(BF16)
-    cache._keep[3].fill_(79)
+    cache.lens.fill_(79)
     out = cache.bd_k_kv8_attention(q, torch.empty_like(q), CAUSAL)
     want, tol = plain_attention(q[0].double().cpu().numpy(), plain.v[0, :80], plain.v[1, :80], 79, CAUSAL, 0, 0, D ** -0.5)
     assert (np.abs(out[0].double().cpu().numpy() - want) <= tol).all()
@@ -524,7 +524,7 @@ def test_rope_with_a_position_for_each_row():
 
 def layer(cache, plan, qkv, turned, out, n_q, n_kv, mode, rows=None, workspace=None):
     """One layer's attention part: the heads of Q and K turned, K and V into the cache, attention."""
-    binding.bd_k_rope(plan, qkv[:, :, :n_q + n_kv], cache._keep[3], out=turned, rows=rows)
+    binding.bd_k_rope(plan, qkv[:, :, :n_q + n_kv], cache.lens, out=turned, rows=rows)
     cache.bd_k_kv8_write(turned[:, :, n_q:], qkv[:, :, n_q + n_kv:], rows=rows)
     cache.bd_k_kv8_attention(turned[:, :, :n_q], out, mode, rows=rows, workspace=workspace)
 
