@@ -59,185 +59,215 @@ template <> __device__ inline u16 from_f32<u16>(float x) {
   return v.u;
 }
 
-// ---- write --------------------------------------------------------------------------------------------------------------
-// One workgroup of 2 D threads per (touched block, head, keys or values).  A thread holds 16 of the block's elements in registers: of the keys
-// eight dimensions of two tokens (eight bytes of the page each), of the values eight tokens of two dimensions (likewise).
-// Bound by the rows' bytes; the block's maximum is one reduction over the workgroup between the load and the store.
-struct Kv8WriteArgs {
+// ---- write and read -------------------------------------------------------------------------------------------------------
+// One wavefront per (block, head, keys or values), two blocks with heads of 64.  A lane has a patch of eight tokens (8 g ..) by eight dimensions:
+// rows move 16 bytes a lane and a token (256 or 128 contiguous bytes a row), and of the page the lane owns whole 16-byte pieces, the keys' after
+// an exchange with its neighbour, the values' after transposing bytes in registers.  Nothing crosses the wavefront: the
+// block's maximum is a reduction over its lanes.  Bound by the rows' bytes.
+struct Kv8CopyArgs {
   bd_kv8 c;
   Kv8Rows r;
-  const void* x[2];
-  int64_t seq_stride[2], row_stride[2];                // of keys, of values
-};
-
-template <int D, typename T>
-__global__ __launch_bounds__(2 * D) void kv8_write_kernel(Kv8WriteArgs a) {
-  __shared__ uint32_t s_max[2 * D / 64], s_nan[2 * D / 64];
-  const int s = blockIdx.z, h = blockIdx.y >> 1, kv = blockIdx.y & 1;
-  int n, rows;
-  if (!kv8_take(a.c, a.r, s, n, rows)) return;
-  const int kb = n / 32 + blockIdx.x;
-  const int lo = max(n - kb * 32, 0), hi = min(n + rows - kb * 32, 32);     // tokens [lo, hi) of the block are new, those before stay
-  if (hi <= lo) return;
-  const int page = kv8_page(a.c, s, kb);
-  if (page < 0) return;
-  const size_t ph = (size_t)page * a.c.n_kv + h;
-  uint8_t* base = a.c.dev_codes + ph * (64 * D);
-  const int tid = threadIdx.x;
-  const int64_t row_stride = a.row_stride[kv];
-  const T* x = reinterpret_cast<const T*>(a.x[kv]) + s * a.seq_stride[kv] + (kb * 32 - n) * row_stride + h * D;
-  const int e_old = lo > 0 ? kv8_byte_exponent(a.c.dev_scales[ph] >> (8 * kv)) : kv8_e_min;
-  float y[2][8];
-  uint8_t* at[2];
-  int tok[2][2];                                       // first token of group j, and its step from element to element
-  if (kv == 0) {
-    const int d = (tid % (D / 8)) * 8;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int t = tid / (D / 8) + 16 * j;
-      tok[j][0] = t; tok[j][1] = 0;
-      at[j] = base + kv8_k_byte(t, d, D);
-      if (t >= lo && t < hi) {
-        constexpr int N = 16 / sizeof(T);
-#pragma unroll
-        for (int q = 0; q < 8 / N; ++q) {
-          const Pack<T, N> p = *reinterpret_cast<const Pack<T, N>*>(x + t * row_stride + d + q * N);
-#pragma unroll
-          for (int i = 0; i < N; ++i) y[j][q * N + i] = to_f32(p.x[i]);
-        }
-      }
-    }
-  } else {
-    const int d = (tid % (D / 2)) * 2, g = tid / (D / 2);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int t = 8 * g + i;
-      if (t >= lo && t < hi) {
-        const Pack<T, 2> p = *reinterpret_cast<const Pack<T, 2>*>(x + t * row_stride + d);
-        y[0][i] = to_f32(p.x[0]);
-        y[1][i] = to_f32(p.x[1]);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      tok[j][0] = 8 * g; tok[j][1] = 1;
-      at[j] = base + 32 * D + kv8_v_byte(8 * g, d + j);
-    }
-  }
-  uint32_t amax = 0;
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int t = tok[j][0] + tok[j][1] * i;
-      const uint32_t u = __float_as_uint(y[j][i]) & 0x7FFFFFFFu;
-      if (t >= lo && t < hi && u < 0x7F800000u) amax = max(amax, u);        // (finite ones; their bits order them)
-    }
-#pragma unroll
-  for (int w = 32; w >= 1; w >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, w, 64));
-  if ((tid & 63) == 0) s_max[tid >> 6] = amax;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 2 * D / 64; ++w) amax = max(amax, s_max[w]);
-  const int e = max(kv8_exponent(amax), e_old);
-  const float down = two_to(-e), again = two_to(max(e_old - e, -126));      // (a smaller one would give 0 all the same)
-  bool nan = false;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    float old[8];
-    const bool any_old = tok[j][0] < lo;
-    if (any_old) {
-      const uint2 w = *reinterpret_cast<const uint2*>(at[j]);
-      decode4(w.x, old);
-      decode4(w.y, old + 4);
-    }
-    float z[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int t = tok[j][0] + tok[j][1] * i;
-      z[i] = t >= hi ? 0.f : t >= lo ? y[j][i] * down : old[i] * again;
-      nan |= z[i] != z[i];
-    }
-    *reinterpret_cast<uint2*>(at[j]) = make_uint2(encode4(z), encode4(z + 4));
-  }
-  uint8_t* word = reinterpret_cast<uint8_t*>(a.c.dev_scales + ph);          // keys and values have bytes of their own
-  if (kv == 0) {
-    if (tid == 0) word[0] = (uint8_t)(e + 127);
-    return;
-  }
-  const unsigned long long b = __builtin_amdgcn_ballot_w64(nan);
-  if ((tid & 63) == 0) s_nan[tid >> 6] = b != 0ull;
-  __syncthreads();
-  if (tid == 0) {
-    uint32_t f = 0;
-#pragma unroll
-    for (int w = 0; w < 2 * D / 64; ++w) f |= s_nan[w];
-    word[1] = (uint8_t)(e + 127);
-    word[2] = (uint8_t)f;
-    word[3] = 0;
-  }
-}
-
-// ---- read ---------------------------------------------------------------------------------------------------------------
-struct Kv8ReadArgs {
-  bd_kv8 c;
-  Kv8Rows r;
-  void* x[2];
+  void* x[2];                                          // keys, values
   int64_t seq_stride[2], row_stride[2];
 };
 
-template <int D, typename T>
-__global__ __launch_bounds__(2 * D) void kv8_read_kernel(Kv8ReadArgs a) {
-  const int s = blockIdx.z, h = blockIdx.y >> 1, kv = blockIdx.y & 1;
+template <int D>
+struct Kv8Patch {
+  int lane, h, kv, g, d;                               // head, keys or values, tokens 8 g .., dimensions d ..
+  int lo, hi, first;                                   // tokens [lo, hi) of the block are the call's, row r is token r - first
+  bool on;                                             // there is something to do, and a page for it
+  size_t ph;                                           // page and head
+  uint8_t* codes;
+  __device__ inline int k_byte(int t) const { return kv8_k_byte(t, d, D); }
+  __device__ inline int v_byte() const { return 32 * D + kv8_v_byte(8 * g, d); }       // 64 bytes: piece r holds dimensions d + r and d + 4 + r
+};
+// False (for the whole wavefront): nothing to do.
+template <int D>
+__device__ inline bool kv8_patch(const Kv8CopyArgs& a, Kv8Patch<D>& p, int& s) {
+  constexpr int per = D / 8, U = 128 / D;              // lanes of a row, blocks of a wavefront
+  p.lane = threadIdx.x & 63;
+  const int u = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int hk = u % (2 * a.c.n_kv);
+  p.h = hk >> 1;
+  p.kv = hk & 1;
+  p.g = (p.lane / per) & 3;
+  p.d = (p.lane % per) * 8;
+  s = blockIdx.z;
   int n, rows;
-  if (!kv8_take(a.c, a.r, s, n, rows)) return;
-  const int kb = n / 32 + blockIdx.x;
-  const int lo = max(n - kb * 32, 0), hi = min(n + rows - kb * 32, 32);
-  if (hi <= lo) return;
-  const int page = kv8_page(a.c, s, kb);
-  if (page < 0) return;
-  const size_t ph = (size_t)page * a.c.n_kv + h;
-  const uint8_t* base = a.c.dev_codes + ph * (64 * D);
-  const int tid = threadIdx.x;
-  const int64_t row_stride = a.row_stride[kv];
-  T* x = reinterpret_cast<T*>(a.x[kv]) + s * a.seq_stride[kv] + (kb * 32 - n) * row_stride + h * D;
-  const float up = two_to(kv8_byte_exponent(a.c.dev_scales[ph] >> (8 * kv)));
-  if (kv == 0) {
-    const int d = (tid % (D / 8)) * 8;
+  if (!kv8_take(a.c, a.r, s, n, rows)) return false;
+  const int kb = n / 32 + (u / (2 * a.c.n_kv)) * U + p.lane / (4 * per);
+  p.first = n - kb * 32;
+  p.lo = max(p.first, 0);
+  p.hi = (int)min((int64_t)n + rows - (int64_t)kb * 32, (int64_t)32);
+  const int page = p.hi > p.lo ? kv8_page(a.c, s, kb) : -1;
+  p.on = page >= 0;
+  p.ph = (size_t)max(page, 0) * a.c.n_kv + p.h;
+  p.codes = a.c.dev_codes + p.ph * (64 * D);
+  return __builtin_amdgcn_ballot_w64(p.on) != 0ull;
+}
+
+// 4 x 4 bytes: byte j of word i and byte i of word j change places.
+__device__ inline void transpose4(uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
+  const uint32_t t0 = __builtin_amdgcn_perm(b, a, 0x05010400u), t1 = __builtin_amdgcn_perm(b, a, 0x07030602u);      // a0 b0 a1 b1, a2 b2 a3 b3
+  const uint32_t t2 = __builtin_amdgcn_perm(d, c, 0x05010400u), t3 = __builtin_amdgcn_perm(d, c, 0x07030602u);
+  a = __builtin_amdgcn_perm(t2, t0, 0x05040100u);
+  b = __builtin_amdgcn_perm(t2, t0, 0x07060302u);
+  c = __builtin_amdgcn_perm(t3, t1, 0x05040100u);
+  d = __builtin_amdgcn_perm(t3, t1, 0x07060302u);
+}
+// The values' patch, w[token][dimensions d .. d + 3 or d + 4 .. d + 7], to and from the page's order.
+__device__ inline void transpose_patch(uint32_t (&w)[8][2]) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int t = tid / (D / 8) + 16 * j;
-      if (t < lo || t >= hi) continue;
-      const uint2 w = *reinterpret_cast<const uint2*>(base + kv8_k_byte(t, d, D));
-      float y[8];
-      decode4(w.x, y);
-      decode4(w.y, y + 4);
-      constexpr int N = 16 / sizeof(T);
+  for (int u = 0; u < 2; ++u) {
+    transpose4(w[0][u], w[1][u], w[2][u], w[3][u]);
+    transpose4(w[4][u], w[5][u], w[6][u], w[7][u]);
+  }
+}
+__device__ inline void load_values(const uint8_t* from, uint32_t (&w)[8][2]) {
 #pragma unroll
-      for (int q = 0; q < 8 / N; ++q) {
-        Pack<T, N> p;
+  for (int r = 0; r < 4; ++r) {
+    const uint4 v = reinterpret_cast<const uint4*>(from)[r];
+    w[r][0] = v.x; w[4 + r][0] = v.y; w[r][1] = v.z; w[4 + r][1] = v.w;
+  }
+  transpose_patch(w);
+}
+
+template <int D, typename T>
+__global__ __launch_bounds__(256) void kv8_write_kernel(Kv8CopyArgs a) {
+  Kv8Patch<D> p;
+  int s;
+  if (!kv8_patch<D>(a, p, s)) return;
+  const int64_t row_stride = a.row_stride[p.kv];
+  const T* x = reinterpret_cast<const T*>(a.x[p.kv]) + s * a.seq_stride[p.kv] + p.h * D + p.d;
+  constexpr int N = 16 / sizeof(T);
+  float y[8][8];
+  uint32_t amax = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) p.x[i] = from_f32<T>(y[q * N + i] * up);
-        *reinterpret_cast<Pack<T, N>*>(x + t * row_stride + d + q * N) = p;
+  for (int i = 0; i < 8; ++i) {
+    const int t = 8 * p.g + i;
+#pragma unroll
+    for (int q = 0; q < 8 / N; ++q) {
+      Pack<T, N> v{};
+      if (p.on && t >= p.lo && t < p.hi) v = *reinterpret_cast<const Pack<T, N>*>(x + (t - p.first) * row_stride + q * N);
+#pragma unroll
+      for (int e = 0; e < N; ++e) y[i][q * N + e] = to_f32(v.x[e]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t u = __float_as_uint(y[i][e]) & 0x7FFFFFFFu;
+      amax = max(amax, u < 0x7F800000u ? u : 0u);                           // (finite ones; their bits order them)
+    }
+#pragma unroll
+  for (int w = D / 4; w >= 1; w >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, w, 64));
+  int e_old = kv8_e_min;
+  if (p.on && p.lo > 0) e_old = kv8_byte_exponent(a.c.dev_scales[p.ph] >> (8 * p.kv));
+  const int e = max(kv8_exponent(amax), e_old);
+  const float down = two_to(-e);
+  uint32_t w[8][2];
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      y[i][q] *= down;
+      nan |= y[i][q] != y[i][q];
+    }
+    w[i][0] = encode4(y[i]);
+    w[i][1] = encode4(y[i] + 4);
+  }
+  if (p.on && 8 * p.g < p.lo) {                        // positions from before among the patch's, encoded again
+    uint32_t old[8][2];
+    if (p.kv == 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p.codes + p.k_byte(8 * p.g + i));
+        old[i][0] = v.x; old[i][1] = v.y;
       }
+    } else {
+      load_values(p.codes + p.v_byte(), old);
     }
-  } else {
-    const int d = (tid % (D / 2)) * 2, g = tid / (D / 2);
-    float y[2][8];
+    const float again = two_to(max(e_old - e, -126));                       // (a smaller one would give 0 all the same)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint2 w = *reinterpret_cast<const uint2*>(base + 32 * D + kv8_v_byte(8 * g, d + j));
-      decode4(w.x, y[j]);
-      decode4(w.y, y[j] + 4);
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float z[4];
+        decode4(old[i][u], z);
+        bool bad = false;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          z[q] *= again;
+          bad |= z[q] != z[q];
+        }
+        if (8 * p.g + i < p.lo) {
+          w[i][u] = encode4(z);
+          nan |= bad;
+        }
+      }
+  }
+  uint8_t* word = reinterpret_cast<uint8_t*>(a.c.dev_scales + p.ph);        // keys and values have bytes of their own
+  constexpr unsigned long long half = D == 128 ? ~0ull : 0xFFFFFFFFull;     // the lanes of one block
+  const unsigned long long nans = __builtin_amdgcn_ballot_w64(nan) >> (p.lane & (64 - D / 2));
+  if (p.kv == 0) {
+    const bool odd = p.lane & 1;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t got[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) got[u] = __builtin_amdgcn_mov_dpp(odd ? w[2 * k][u] : w[2 * k + 1][u], 0xB1, 0xF, 0xF, true);      // from lane ^ 1
+      const uint4 v = odd ? make_uint4(got[0], got[1], w[2 * k + 1][0], w[2 * k + 1][1]) : make_uint4(w[2 * k][0], w[2 * k][1], got[0], got[1]);
+      if (p.on) *reinterpret_cast<uint4*>(p.codes + kv8_k_byte(8 * p.g + 2 * k + odd, p.d & ~15, D)) = v;
     }
+    if (p.on && (p.lane & (D / 2 - 1)) == 0) word[0] = (uint8_t)(e + 127);
+  } else {
+    transpose_patch(w);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (p.on) reinterpret_cast<uint4*>(p.codes + p.v_byte())[r] = make_uint4(w[r][0], w[4 + r][0], w[r][1], w[4 + r][1]);
+    if (p.on && (p.lane & (D / 2 - 1)) == 0) {
+      word[1] = (uint8_t)(e + 127);
+      word[2] = (nans & half) != 0ull;
+      word[3] = 0;
+    }
+  }
+}
+
+template <int D, typename T>
+__global__ __launch_bounds__(256) void kv8_read_kernel(Kv8CopyArgs a) {
+  Kv8Patch<D> p;
+  int s;
+  if (!kv8_patch<D>(a, p, s)) return;
+  if (!p.on || 8 * p.g >= p.hi || 8 * p.g + 8 <= p.lo) return;
+  const int64_t row_stride = a.row_stride[p.kv];
+  T* x = reinterpret_cast<T*>(a.x[p.kv]) + s * a.seq_stride[p.kv] + p.h * D + p.d;
+  uint32_t w[8][2];
+  if (p.kv == 0) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int t = 8 * g + i;
-      if (t < lo || t >= hi) continue;
-      Pack<T, 2> p;
-      p.x[0] = from_f32<T>(y[0][i] * up);
-      p.x[1] = from_f32<T>(y[1][i] * up);
-      *reinterpret_cast<Pack<T, 2>*>(x + t * row_stride + d) = p;
+      const uint2 v = *reinterpret_cast<const uint2*>(p.codes + p.k_byte(8 * p.g + i));
+      w[i][0] = v.x; w[i][1] = v.y;
+    }
+  } else {
+    load_values(p.codes + p.v_byte(), w);
+  }
+  const float up = two_to(kv8_byte_exponent(a.c.dev_scales[p.ph] >> (8 * p.kv)));
+  constexpr int N = 16 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int t = 8 * p.g + i;
+    float y[8];
+    decode4(w[i][0], y);
+    decode4(w[i][1], y + 4);
+    if (t < p.lo || t >= p.hi) continue;
+#pragma unroll
+    for (int q = 0; q < 8 / N; ++q) {
+      Pack<T, N> v;
+#pragma unroll
+      for (int e = 0; e < N; ++e) v.x[e] = from_f32<T>(y[q * N + e] * up);
+      *reinterpret_cast<Pack<T, N>*>(x + (t - p.first) * row_stride + q * N) = v;
     }
   }
 }
@@ -598,37 +628,57 @@ struct RopeArgs {
   int heads, M;
 };
 
-// One workgroup per row: sines and cosines of the row's angles once for all heads (fp64 up to the reduced angle: at position 2^20 an
-// angle in fp32 is off by up to 2^-5), then the heads, a pair at a time.
-template <typename T>
-__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  __shared__ float s_cos[64], s_sin[64];
-  const int s = blockIdx.y, r = blockIdx.x;
-  const int rows = a.rows != nullptr ? a.rows[s] : a.M;
-  if (r >= rows) return;
-  const int R2 = a.plan.rotary_dim >> 1, D = a.plan.D, tid = threadIdx.x;
-  if (tid < R2) {
-    const double turns = ((double)a.pos[s] + r) * a.plan.inv_freq[tid] * 0.15915494309189533577;   // 1/(2 pi)
+// A workgroup takes `per` rows: sines and cosines of their angles once for all heads (fp64 up to the reduced angle: at position 2^20 an
+// angle in fp32 is off by up to 2^-5), then the heads.  Bound by the rows' bytes: 16 a lane and access, VEC, where the two halves of a rotary part
+// fall on 16 bytes (with neighbouring pairs always), else an element at a time.
+constexpr int kRopeRows = 4;
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int per) {
+  __shared__ float2 s_cs[kRopeRows][64];               // (cosine, sine)
+  const int s = blockIdx.y, r0 = blockIdx.x * per, tid = threadIdx.x;
+  const int rows = min(a.rows != nullptr ? a.rows[s] : a.M, a.M) - r0, n = min(rows, per);
+  if (n <= 0) return;
+  const int R2 = a.plan.rotary_dim >> 1, D = a.plan.D;
+  if (tid < 64 * n && (tid & 63) < R2) {
+    const double turns = ((double)a.pos[s] + (r0 + (tid >> 6))) * a.plan.inv_freq[tid & 63] * 0.15915494309189533577;   // 1/(2 pi)
     float sn, cs;
     sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
-    s_cos[tid] = cs * a.plan.amplitude;
-    s_sin[tid] = sn * a.plan.amplitude;
+    s_cs[tid >> 6][tid & 63] = make_float2(cs * a.plan.amplitude, sn * a.plan.amplitude);
   }
   __syncthreads();
-  const T* x = reinterpret_cast<const T*>(a.x) + s * a.x_seq + r * a.x_row;
-  T* y = reinterpret_cast<T*>(a.y) + s * a.y_seq + r * a.y_row;
-  const bool half = a.plan.layout == BD_ROPE_HALF;
-  for (int i = tid; i < a.heads * (D >> 1); i += 256) {
-    const int h = i / (D >> 1), j = i % (D >> 1);
-    if (j < R2) {
-      const int d0 = h * D + (half ? j : 2 * j), d1 = h * D + (half ? j + R2 : 2 * j + 1);
-      const float u = to_f32(x[d0]), v = to_f32(x[d1]), c = s_cos[j], sn = s_sin[j];
-      y[d0] = from_f32<T>(u * c - v * sn);
-      y[d1] = from_f32<T>(v * c + u * sn);
-    } else {
-      y[h * D + 2 * j] = x[h * D + 2 * j];
-      y[h * D + 2 * j + 1] = x[h * D + 2 * j + 1];
+  const T* x = reinterpret_cast<const T*>(a.x) + s * a.x_seq + r0 * a.x_row;
+  T* y = reinterpret_cast<T*>(a.y) + s * a.y_seq + r0 * a.y_row;
+  const bool half = a.plan.layout == BD_ROPE_HALF, in_place = a.x == a.y;
+  constexpr int N = VEC ? 16 / sizeof(T) : 1;
+  typedef Pack<T, N> V;
+  // an item: two vectors of a head whose elements make pairs (half), or that lie side by side (neighbouring pairs and the rest of the head)
+  const int item_log = (D == 128 ? 6 : 5) - (N == 8 ? 3 : N == 4 ? 2 : 0), items = a.heads << item_log;
+  for (int i = tid; i < n * items; i += 256) {
+    const int r = i / items, k = i % items, h = k >> item_log, j = k & ((1 << item_log) - 1);
+    const bool turn = j * N < R2;
+    if (in_place && !turn) continue;
+    const int d0 = h * D + (half && turn ? j * N : 2 * j * N), d1 = half && turn ? d0 + R2 : d0 + N;
+    const V u = *reinterpret_cast<const V*>(x + r * a.x_row + d0), v = *reinterpret_cast<const V*>(x + r * a.x_row + d1);
+    V p = u, q = v;
+    if (turn) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        // half: pair (u[e], v[e]); neighbours: pairs lie along u, then v
+        const float2 cs = s_cs[r][min(j * N + e, 63)];
+        if (half || N == 1) {
+          const float b0 = to_f32(u.x[e]), b1 = to_f32(v.x[e]);
+          p.x[e] = from_f32<T>(b0 * cs.x - b1 * cs.y);
+          q.x[e] = from_f32<T>(b1 * cs.x + b0 * cs.y);
+        } else if (j * N + e < R2) {
+          const int at = (2 * e) % N;
+          const float b0 = to_f32(2 * e < N ? u.x[at] : v.x[at]), b1 = to_f32(2 * e < N ? u.x[at + (N > 1)] : v.x[at + (N > 1)]);
+          (2 * e < N ? p : q).x[at] = from_f32<T>(b0 * cs.x - b1 * cs.y);
+          (2 * e < N ? p : q).x[at + (N > 1)] = from_f32<T>(b1 * cs.x + b0 * cs.y);
+        }
+      }
     }
+    *reinterpret_cast<V*>(y + r * a.y_row + d0) = p;
+    *reinterpret_cast<V*>(y + r * a.y_row + d1) = q;
   }
 }
 
@@ -662,9 +712,11 @@ int blocks_of(int M, int max_blocks) {
   return b < max_blocks ? b : max_blocks;
 }
 
-template <typename A, typename K>
-int launch_blocks(hipStream_t s, K kernel, int D, const bd_kv8& c, int M, const A& a) {
-  hipLaunchKernelGGL(kernel, dim3(blocks_of(M, c.max_blocks), 2 * c.n_kv, c.n_seq), dim3(2 * D), 0, s, a);
+template <typename K>
+int launch_copy(hipStream_t s, K kernel, const Kv8CopyArgs& a) {
+  const int64_t wavefronts = (int64_t)ceil_div(blocks_of(a.r.M, a.c.max_blocks), 128 / a.c.D) * 2 * a.c.n_kv;
+  if (wavefronts >= ((int64_t)1 << 26)) return BD_E_ARG;      // (2^32 threads are one too many for a launch)
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((wavefronts + 3) / 4), 1, a.c.n_seq), dim3(256), 0, s, a);
   return check_launch();
 }
 
@@ -710,10 +762,9 @@ extern "C" int bd_k_kv8_write(void* hip_stream, const bd_kv8* cache, const void*
   BD_TRY(check_rows(dev_v, dtype, v_seq_stride, v_row_stride, cache->n_seq, M));
   if (cache->dev_len == nullptr) return BD_E_ARG;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const Kv8WriteArgs a{*cache, {cache->dev_len, dev_rows, M}, {dev_k, dev_v}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}};
-  if (cache->D == 128)
-    return dtype == BD_F32 ? launch_blocks(s, kv8_write_kernel<128, float>, 128, *cache, M, a) : launch_blocks(s, kv8_write_kernel<128, u16>, 128, *cache, M, a);
-  return dtype == BD_F32 ? launch_blocks(s, kv8_write_kernel<64, float>, 64, *cache, M, a) : launch_blocks(s, kv8_write_kernel<64, u16>, 64, *cache, M, a);
+  const Kv8CopyArgs a{*cache, {cache->dev_len, dev_rows, M}, {const_cast<void*>(dev_k), const_cast<void*>(dev_v)}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}};
+  if (cache->D == 128) return dtype == BD_F32 ? launch_copy(s, kv8_write_kernel<128, float>, a) : launch_copy(s, kv8_write_kernel<128, u16>, a);
+  return dtype == BD_F32 ? launch_copy(s, kv8_write_kernel<64, float>, a) : launch_copy(s, kv8_write_kernel<64, u16>, a);
 }
 
 extern "C" int bd_k_kv8_read(void* hip_stream, const bd_kv8* cache, const int32_t* dev_from, int M, const int32_t* dev_rows, int dtype,
@@ -724,10 +775,9 @@ extern "C" int bd_k_kv8_read(void* hip_stream, const bd_kv8* cache, const int32_
   BD_TRY(check_rows(dev_k_out, dtype, k_seq_stride, k_row_stride, cache->n_seq, M, least));
   BD_TRY(check_rows(dev_v_out, dtype, v_seq_stride, v_row_stride, cache->n_seq, M, least));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const Kv8ReadArgs a{*cache, {dev_from, dev_rows, M}, {dev_k_out, dev_v_out}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}};
-  if (cache->D == 128)
-    return dtype == BD_F32 ? launch_blocks(s, kv8_read_kernel<128, float>, 128, *cache, M, a) : launch_blocks(s, kv8_read_kernel<128, u16>, 128, *cache, M, a);
-  return dtype == BD_F32 ? launch_blocks(s, kv8_read_kernel<64, float>, 64, *cache, M, a) : launch_blocks(s, kv8_read_kernel<64, u16>, 64, *cache, M, a);
+  const Kv8CopyArgs a{*cache, {dev_from, dev_rows, M}, {dev_k_out, dev_v_out}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}};
+  if (cache->D == 128) return dtype == BD_F32 ? launch_copy(s, kv8_read_kernel<128, float>, a) : launch_copy(s, kv8_read_kernel<128, u16>, a);
+  return dtype == BD_F32 ? launch_copy(s, kv8_read_kernel<64, float>, a) : launch_copy(s, kv8_read_kernel<64, u16>, a);
 }
 
 extern "C" int64_t bd_k_kv8_attention_workspace(const bd_kv8* cache, int n_q, int M, int window, int sinks) {
@@ -799,12 +849,22 @@ extern "C" int bd_k_rope(void* hip_stream, const bd_rope* plan, const void* dev_
   if (n_heads < 1 || n_heads > (1 << 16) || n_seq < 1 || n_seq > 65535 || M < 1 || M > kMaxRows || dev_pos == nullptr) return BD_E_ARG;
   BD_TRY(check_rows(dev_x, dtype, x_seq_stride, x_row_stride, n_seq, M));
   BD_TRY(check_rows(dev_out, dtype, out_seq_stride, out_row_stride, n_seq, M, (int64_t)n_heads * plan->D));
+  if (dev_x == dev_out && ((n_seq > 1 && x_seq_stride != out_seq_stride) || (M > 1 && x_row_stride != out_row_stride))) return BD_E_ARG;
   RopeArgs a{};
   a.plan = *plan;
   a.x = dev_x; a.y = dev_out; a.x_seq = x_seq_stride; a.x_row = x_row_stride; a.y_seq = out_seq_stride; a.y_row = out_row_stride;
   a.pos = dev_pos; a.rows = dev_rows; a.heads = n_heads; a.M = M;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (dtype == BD_F32) hipLaunchKernelGGL((rope_kernel<float>), dim3(M, n_seq), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((rope_kernel<u16>), dim3(M, n_seq), dim3(256), 0, s, a);
+  const int N = dtype == BD_F32 ? 4 : 8;
+  const bool vec = plan->layout == BD_ROPE_INTERLEAVED || plan->rotary_dim % (2 * N) == 0;
+  const int per = (int64_t)M * n_seq >= 4096 ? kRopeRows : 1;               // few rows: a workgroup each
+  const dim3 grid(ceil_div(M, per), n_seq);
+  if (dtype == BD_F32) {
+    if (vec) hipLaunchKernelGGL((rope_kernel<float, true>), grid, dim3(256), 0, s, a, per);
+    else hipLaunchKernelGGL((rope_kernel<float, false>), grid, dim3(256), 0, s, a, per);
+  } else {
+    if (vec) hipLaunchKernelGGL((rope_kernel<u16, true>), grid, dim3(256), 0, s, a, per);
+    else hipLaunchKernelGGL((rope_kernel<u16, false>), grid, dim3(256), 0, s, a, per);
+  }
   return check_launch();
 }

@@ -179,6 +179,7 @@ static void refusals() {
   CHECK(rope(nullptr) == BD_E_ARG && rope(&p, nullptr) == BD_E_ARG && rope(&p, mem + 4) == BD_E_ARG && rope(&p, mem, 130) == BD_E_ARG && rope(&p, mem, 128, 9) == BD_E_DTYPE);
   CHECK(rope(&p, mem, 128, BD_F32, 0) == BD_E_ARG && rope(&p, mem, 128, BD_F32, 2) == BD_E_ARG && rope(&p, mem, 128, BD_F32, 1, 0) == BD_E_ARG &&
         rope(&p, mem, 128, BD_F32, 1, 1, 0) == BD_E_ARG && rope(&p, mem, 128, BD_F32, 1, 1, 2, nullptr) == BD_E_ARG);
+  CHECK(rope(&p, mem, 192) == BD_E_ARG);                     // in place with another stride
   for (auto f : {+[](bd_rope& x) { x.D = 32; }, +[](bd_rope& x) { x.rotary_dim = 130; }, +[](bd_rope& x) { x.rotary_dim = 7; }, +[](bd_rope& x) { x.layout = 5; }}) {
     bd_rope x = p;
     f(x);
