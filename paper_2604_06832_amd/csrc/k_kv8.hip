@@ -74,14 +74,14 @@ struct Kv8CopyArgs {
 template <int D>
 struct Kv8Patch {
   int lane, h, kv, g, d;                               // head, keys or values, tokens 8 g .., dimensions d ..
-  int lo, hi, first;                                   // tokens [lo, hi) of the block are the call's, row r is token r - first
+  int kb, lo, hi, first;                               // block; tokens [lo, hi) of the block are the call's, row r is token r - first
   bool on;                                             // there is something to do, and a page for it
   size_t ph;                                           // page and head
   uint8_t* codes;
   __device__ inline int k_byte(int t) const { return kv8_k_byte(t, d, D); }
   __device__ inline int v_byte() const { return 32 * D + kv8_v_byte(8 * g, d); }       // 64 bytes: piece r holds dimensions d + r and d + 4 + r
 };
-// False (for the whole wavefront): nothing to do.
+// Where the patch lies; false (for the whole wavefront): nothing to do.
 template <int D>
 __device__ inline bool kv8_patch(const Kv8CopyArgs& a, Kv8Patch<D>& p, int& s) {
   constexpr int per = D / 8, U = 128 / D;              // lanes of a row, blocks of a wavefront
@@ -99,11 +99,17 @@ __device__ inline bool kv8_patch(const Kv8CopyArgs& a, Kv8Patch<D>& p, int& s) {
   p.first = n - kb * 32;
   p.lo = max(p.first, 0);
   p.hi = (int)min((int64_t)n + rows - (int64_t)kb * 32, (int64_t)32);
-  const int page = p.hi > p.lo ? kv8_page(a.c, s, kb) : -1;
+  p.on = p.hi > p.lo;
+  p.kb = kb;
+  return __builtin_amdgcn_ballot_w64(p.on) != 0ull;
+}
+// Its page.
+template <int D>
+__device__ inline void kv8_patch_page(const Kv8CopyArgs& a, Kv8Patch<D>& p, int s) {
+  const int page = p.on ? kv8_page(a.c, s, p.kb) : -1;
   p.on = page >= 0;
   p.ph = (size_t)max(page, 0) * a.c.n_kv + p.h;
   p.codes = a.c.dev_codes + p.ph * (64 * D);
-  return __builtin_amdgcn_ballot_w64(p.on) != 0ull;
 }
 
 // 4 x 4 bytes: byte j of word i and byte i of word j change places.
@@ -139,31 +145,45 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8CopyArgs a) {
   if (!kv8_patch<D>(a, p, s)) return;
   const int64_t row_stride = a.row_stride[p.kv];
   const T* x = reinterpret_cast<const T*>(a.x[p.kv]) + s * a.seq_stride[p.kv] + p.h * D + p.d;
+  // all loads before the first wait: the rows, then the page's word and the codes that stay
   constexpr int N = 16 / sizeof(T);
-  float y[8][8];
-  uint32_t amax = 0;
+  Pack<T, N> raw[8][8 / N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int t = 8 * p.g + i;
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int q = 0; q < 8 / N; ++q) {
-      Pack<T, N> v{};
-      if (p.on && t >= p.lo && t < p.hi) v = *reinterpret_cast<const Pack<T, N>*>(x + (t - p.first) * row_stride + q * N);
+      const int t = 8 * p.g + i;
+      raw[i][q] = Pack<T, N>{};
+      if (p.on && t >= p.lo && t < p.hi) raw[i][q] = *reinterpret_cast<const Pack<T, N>*>(x + (t - p.first) * row_stride + q * N);
+    }
+  kv8_patch_page<D>(a, p, s);
+  int e_old = kv8_e_min;
+  const bool keeps = p.on && 8 * p.g < p.lo;           // positions from before among the patch's: encoded again
+  uint32_t old[8][2] = {};
+  if (p.on && p.lo > 0) {
+    e_old = kv8_byte_exponent(a.c.dev_scales[p.ph] >> (8 * p.kv));
+    if (keeps && p.kv == 0) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) y[i][q * N + e] = to_f32(v.x[e]);
+      for (int i = 0; i < 8; ++i) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p.codes + p.k_byte(8 * p.g + i));
+        old[i][0] = v.x; old[i][1] = v.y;
+      }
+    } else if (keeps) {
+      load_values(p.codes + p.v_byte(), old);
     }
   }
+  float y[8][8];
+  uint32_t amax = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+      y[i][e] = to_f32(raw[i][e / N].x[e % N]);
       const uint32_t u = __float_as_uint(y[i][e]) & 0x7FFFFFFFu;
       amax = max(amax, u < 0x7F800000u ? u : 0u);                           // (finite ones; their bits order them)
     }
 #pragma unroll
   for (int w = D / 4; w >= 1; w >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, w, 64));
-  int e_old = kv8_e_min;
-  if (p.on && p.lo > 0) e_old = kv8_byte_exponent(a.c.dev_scales[p.ph] >> (8 * p.kv));
   const int e = max(kv8_exponent(amax), e_old);
   const float down = two_to(-e);
   uint32_t w[8][2];
@@ -178,17 +198,7 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8CopyArgs a) {
     w[i][0] = encode4(y[i]);
     w[i][1] = encode4(y[i] + 4);
   }
-  if (p.on && 8 * p.g < p.lo) {                        // positions from before among the patch's, encoded again
-    uint32_t old[8][2];
-    if (p.kv == 0) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint2 v = *reinterpret_cast<const uint2*>(p.codes + p.k_byte(8 * p.g + i));
-        old[i][0] = v.x; old[i][1] = v.y;
-      }
-    } else {
-      load_values(p.codes + p.v_byte(), old);
-    }
+  if (keeps) {
     const float again = two_to(max(e_old - e, -126));                       // (a smaller one would give 0 all the same)
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -240,6 +250,7 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8CopyArgs a) {
   Kv8Patch<D> p;
   int s;
   if (!kv8_patch<D>(a, p, s)) return;
+  kv8_patch_page<D>(a, p, s);
   if (!p.on || 8 * p.g >= p.hi || 8 * p.g + 8 <= p.lo) return;
   const int64_t row_stride = a.row_stride[p.kv];
   T* x = reinterpret_cast<T*>(a.x[p.kv]) + s * a.seq_stride[p.kv] + p.h * D + p.d;
@@ -283,6 +294,7 @@ struct Kv8AttnArgs {
   float c_log2;                 // scale * log2(e)
   int tiles, groups, chunks, runs, run_len;
 };
+constexpr int kv8_nowhere = 1 << 25;      // number of a block that is none: past every sequence's end
 constexpr float kv8_lowest = -3.0e38f;   // start of a running maximum: below every finite score, and finite itself
 
 // A block's codes, as the lanes load them.
@@ -294,17 +306,25 @@ template <int D>
 __device__ inline const uint4* kv8_codes(const bd_kv8& c, int page, int h, int lane) {
   return reinterpret_cast<const uint4*>(c.dev_codes + ((size_t)page * c.n_kv + h) * (64 * D)) + lane;
 }
-template <int D>
+// ONCE: they pass the caches by.
+template <bool ONCE>
+__device__ inline uint4 kv8_load(const uint4* p) {
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  if constexpr (!ONCE) return *p;
+  const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+template <int D, bool ONCE>
 __device__ inline void kv8_load_k(Kv8Block<D>& b, const uint4* p) {
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) b.k[t][j] = p[(t * (D / 64) + j) * 64];
+    for (int j = 0; j < D / 64; ++j) b.k[t][j] = kv8_load<ONCE>(p + (t * (D / 64) + j) * 64);
 }
-template <int D>
+template <int D, bool ONCE>
 __device__ inline void kv8_load_v(Kv8Block<D>& b, const uint4* p) {
 #pragma unroll
-  for (int j = 0; j < D / 32; ++j) b.v[j] = p[(D / 32 + j) * 64];
+  for (int j = 0; j < D / 32; ++j) b.v[j] = kv8_load<ONCE>(p + (D / 32 + j) * 64);
 }
 // Eight codes times 2^e as a bf16 operand (exact).
 __device__ inline bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
@@ -335,7 +355,7 @@ __device__ inline bool kv8_visible(const Kv8Cols<JT>& w, const Kv8AttnArgs& a, i
 // blocks need no maximum across lanes.  The sum of the weights is a product too, with a row of ones: what divides the result are the
 // same rounded weights that make it.  Once a block's keys are in operands the next block's are loaded over them, then likewise the values: each
 // load has the other half of a block to arrive.
-template <int D, int JT>
+template <int D, int JT, bool ONCE>
 __device__ inline void kv8_block(Kv8Block<D>& b, uint32_t word, bool clear, const uint4* next, const bf16x8 (&qf)[JT][D / 32], f32x4 (&O)[JT][D / 16], float (&mrun)[JT],
                                  f32x4 (&L)[JT], int kb, const Kv8Cols<JT>& cols, const Kv8AttnArgs& a, int g) {
   constexpr int DT = D / 16;
@@ -356,7 +376,7 @@ __device__ inline void kv8_block(Kv8Block<D>& b, uint32_t word, bool clear, cons
     }
   }
   __builtin_amdgcn_sched_barrier(0);                    // (the loads stay behind the last use of what they overwrite)
-  kv8_load_k<D>(b, next);
+  kv8_load_k<D, ONCE>(b, next);
   if (!clear) {
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt)
@@ -408,7 +428,7 @@ __device__ inline void kv8_block(Kv8Block<D>& b, uint32_t word, bool clear, cons
     for (int jt = 0; jt < JT; ++jt) O[jt][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p8[jt], O[jt][2 * j + 1], 0, 0, 0);
   }
   __builtin_amdgcn_sched_barrier(0);
-  kv8_load_v<D>(b, next);
+  kv8_load_v<D, ONCE>(b, next);
 }
 
 // A block with NaN among its values that not every row sees all of: results become NaN where a row sees one of its dimension.
@@ -450,7 +470,7 @@ __device__ inline void kv8_store(u16* o, const f32x4& a, const f32x4& b, float i
 // read the same blocks, go to one XCD (numbers that differ by multiples of 8), where its L2 serves all but the first, or are dealt to several
 // where there are fewer than 8 such units; the last groups, which see most, start first.
 template <int D, int JT, int NW> constexpr int kv8_attn_lds() { return NW * JT * ((D / 16) * 1024 + 2 * 64); }
-template <int D, int JT, int NW, int AHEAD>
+template <int D, int JT, int NW, int AHEAD, bool ONCE>
 __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
   constexpr int DT = D / 16;
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -478,7 +498,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
   auto look_up = [&](int base) {
     my_page = 0;
     my_word = kv8_v_nan | 0x7F7F;
-    my_kb = 1 << 25;
+    my_kb = kv8_nowhere;
     if (base + lane < cnt) {
       const int idx = first + (base + lane) * step, kb = idx < sp.sink_blocks ? idx : sp.first_block + idx - sp.sink_blocks;
       const int page = kv8_page(a.c, s, kb);
@@ -488,6 +508,8 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
         my_word = a.c.dev_scales[(size_t)page * a.c.n_kv + h];
       }
     }
+    // waited for here: behind a branch that may have left loads open, every later wait would be one for all of them
+    asm volatile("" : "+v"(my_page), "+v"(my_kb), "+v"(my_word));
   };
   look_up(0);
   bf16x8 qf[JT][D / 32];
@@ -526,19 +548,21 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const uint4* codes = next_of(u, kbs[u], words[u]);
-      kv8_load_k<D>(blk[u], codes);
-      kv8_load_v<D>(blk[u], codes);
+      // (in the order in which the loop will ask for them: its first wait has to hold for this entry to it too)
+      __builtin_amdgcn_sched_barrier(0);
+      kv8_load_k<D, ONCE>(blk[u], codes);
+      __builtin_amdgcn_sched_barrier(0);
+      kv8_load_v<D, ONCE>(blk[u], codes);
     }
     for (int i = 0; i < cnt; i += AHEAD) {
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        if (u > 0 && i + u >= cnt) break;
-        const int kb = kbs[u];
+        const int kb = kbs[u];          // (an odd one out is followed by one past the end: a way round it would cost every wait its count)
         const uint32_t word = words[u];
         const bool clear = is_clear(kb);
         const uint4* next = next_of(i + u + AHEAD, kbs[u], words[u]);
-        kv8_block<D, JT>(blk[u], word, clear, next, qf, O, mrun, L, kb, cols, a, g);
-        nan |= !clear && (word & kv8_v_nan) != 0u;
+        kv8_block<D, JT, ONCE>(blk[u], word, clear, next, qf, O, mrun, L, kb, cols, a, g);
+        nan |= !clear && (word & kv8_v_nan) != 0u && kb != kv8_nowhere;
       }
     }
   }
@@ -548,7 +572,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
       int kb;
       uint32_t word;
       const uint4* codes = next_of(i, kb, word);
-      if (!is_clear(kb) && (word & kv8_v_nan) != 0u) kv8_nan_rows<D, JT>(codes, O, kb, cols, a, g);
+      if (!is_clear(kb) && (word & kv8_v_nan) != 0u && kb != kv8_nowhere) kv8_nan_rows<D, JT>(codes, O, kb, cols, a, g);
     }
   }
 #pragma unroll
@@ -720,7 +744,7 @@ int launch_copy(hipStream_t s, K kernel, const Kv8CopyArgs& a) {
   return check_launch();
 }
 
-template <int D, int JT, int NW, int AHEAD>
+template <int D, int JT, int NW, int AHEAD, bool ONCE>
 int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
   constexpr int lds = kv8_attn_lds<D, JT, NW>();
   if (lds > 65536) {
@@ -729,13 +753,13 @@ int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
     HIP_TRY(hipGetDevice(&dev));
     const uint64_t bit = (uint64_t)1 << (dev & 63);
     if (dev > 63 || (allowed.load(std::memory_order_relaxed) & bit) == 0) {
-      HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attn_kernel<D, JT, NW, AHEAD>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+      HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attn_kernel<D, JT, NW, AHEAD, ONCE>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
       if (dev <= 63) allowed.fetch_or(bit, std::memory_order_relaxed);
     }
   }
   const int64_t units = (int64_t)a.c.n_seq * a.c.n_kv * p.chunks, grid = (units * p.runs + 7) / 8 * 8 * p.run_len;
   if (grid * NW * 64 >= ((int64_t)1 << 32)) return BD_E_ARG;
-  hipLaunchKernelGGL((kv8_attn_kernel<D, JT, NW, AHEAD>), dim3((unsigned)grid), dim3(NW * 64), lds, s, a);
+  hipLaunchKernelGGL((kv8_attn_kernel<D, JT, NW, AHEAD, ONCE>), dim3((unsigned)grid), dim3(NW * 64), lds, s, a);
   BD_TRY(check_launch());
   if (p.chunks > 1) {
     hipLaunchKernelGGL((kv8_merge_kernel<D>), dim3((unsigned)((int64_t)a.c.n_seq * a.c.n_kv * p.tiles * (D / 32))), dim3(64), 0, s, a, JT);
@@ -743,6 +767,15 @@ int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
   }
   return BD_OK;
 }
+template <int D>
+int launch_attn_form(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
+  switch (p.form) {
+    case Kv8Form::wide: return launch_attn<D, 2, 4, 2, false>(s, a, p);
+    case Kv8Form::stream: return launch_attn<D, 1, 4, 2, true>(s, a, p);
+    default: return launch_attn<D, 1, 8, 1, false>(s, a, p);
+  }
+}
+
 int check_attn(const bd_kv8* c, int n_q, int M, int window, int sinks, bool shape_only, Kv8Plan* p) {
   BD_TRY(check_cache(c, M, shape_only));
   if (n_q < 1 || n_q > (1 << 16) || n_q % c->n_kv != 0 || window < 0 || sinks < 0) return BD_E_ARG;
@@ -809,8 +842,8 @@ extern "C" int bd_k_kv8_attention(void* hip_stream, const bd_kv8* cache, const v
   a.c_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)cache->D)) * 1.4426950408889634f;
   a.tiles = p.tiles; a.groups = p.groups; a.chunks = p.chunks; a.runs = p.runs; a.run_len = p.run_len;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (cache->D == 128) return p.JT == 2 ? launch_attn<128, 2, 4, 2>(s, a, p) : launch_attn<128, 1, 8, 1>(s, a, p);
-  return p.JT == 2 ? launch_attn<64, 2, 4, 2>(s, a, p) : launch_attn<64, 1, 8, 1>(s, a, p);
+  if (cache->D == 128) return launch_attn_form<128>(s, a, p);
+  return launch_attn_form<64>(s, a, p);
 }
 
 extern "C" int bd_k_rope_plan(bd_rope* out, int D, int rotary_dim, int layout, double theta, int scaling, double factor, int trained) {

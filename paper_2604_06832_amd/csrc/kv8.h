@@ -1,6 +1,7 @@
 // The key/value cache in 8 bits (include/bd_kernels.h): layout of a page, arithmetic of its scales, rules on rows and on what a
 // row sees, and the plan of the attention's launch, shared by host and device.
 #pragma once
+#include <cstdlib>
 #include "../../include/bd_kernels.h"
 #include "common.h"
 
@@ -65,35 +66,43 @@ __host__ __device__ inline bool kv8_sees(int p, int key, int end, int mode, int 
 }
 
 // Launch plan of the attention.  An item is a tile of 16 columns (column = row * G + head of the group) of a (sequence, kv head).
+enum class Kv8Form { walk, wide, stream };   // one tile, eight wavefronts; two tiles, four; one tile, four, past the caches
 struct Kv8Plan {
+  Kv8Form form;
   int tiles;        // of a (sequence, kv head)
-  int JT, NW;       // tiles and wavefronts of a workgroup
+  int JT;           // tiles of a workgroup
   int groups;       // workgroups for a unit: (sequence, kv head, chunk)
   int chunks;       // workgroups that share out the blocks of a group, at most
   int runs, run_len;     // parts of a unit's groups that go to an XCD each, and their length
   int64_t part_floats;   // workspace: unnormalised partial results, [sequence][kv head][tile][chunk]
 };
 constexpr int kv8_chunk_blocks = 32, kv8_cus = 256;
+constexpr int64_t kv8_once_bytes = (int64_t)96 << 20;
 inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_blocks, int window, int sinks) {
   Kv8Plan p{};
   p.tiles = (int)(((int64_t)M * (n_q / n_kv) + 15) / 16);
   const int64_t items = (int64_t)n_seq * n_kv * p.tiles;
-  // More items than CUs: two tiles share each block that a wavefront loads and widens, four wavefronts, two workgroups a CU.  Else one tile and
-  // eight wavefronts, for the shortest walk.  us, (1 tile, 8) and (2 tiles, 4): 256 items behind 2048 keys 13.2 and 18.1, 512 items 25.0 and
-  // 19.8, 1024 rows (1024 items) behind 7168 keys 128 and 73.
-  const bool wide = items > kv8_cus && p.tiles > 1;
-  p.JT = wide ? 2 : 1;
-  p.NW = wide ? 4 : 8;
-  p.groups = ceil_div(p.tiles, p.JT);
-  // Fewer items than CUs: the blocks of an item in chunks of about 32, four a wavefront, as far as there are CUs for them.  us, 1 / 2 / 4 / 8 /
-  // 16 chunks: one row behind 8192 keys 30 / 21 / 15 / 11.9 / 11.7, behind 1024 8.5 / 10.3 / ..; 256 items behind 2048 keys 12.2 / 18.0 / ..
   int64_t blocks = max_blocks;
   if (window > 0) {
     const int64_t w = ((int64_t)window + M + 62) / 32 + 1 + ((int64_t)sinks + 31) / 32;
     if (w < blocks) blocks = w;
   }
+  // One tile and a cache too large for the last-level cache: every block has one reader and will be gone from the caches before its next use, so
+  // its loads pass them by; two blocks ahead, four wavefronts, three workgroups a CU.  us, stream and walk: 64 sequences up to 8192 (137 MB) 35.5 and
+  // 40.1, 256 up to 4096 59 and 66; 32 up to 8192 (66 MB, which stays cached between runs) 27 and 21.  Loads alone take as long as the whole kernel.
+  // More items than CUs: two tiles share each block that a wavefront loads and widens, two blocks ahead, four wavefronts, two workgroups a CU.
+  // Else one tile and eight wavefronts, for the shortest walk.  us, walk and wide: 256 items behind 2048 keys 13.2 and 18.1, 512 items 25.0
+  // and 19.8, 1024 rows (1024 items) behind 7168 keys 128 and 73.
+  const bool once = p.tiles == 1 && (int64_t)n_seq * n_kv * blocks * 64 * D >= kv8_once_bytes;
+  p.form = once ? Kv8Form::stream : items > kv8_cus && p.tiles > 1 ? Kv8Form::wide : Kv8Form::walk;
+  p.JT = p.form == Kv8Form::wide ? 2 : 1;
+  p.groups = ceil_div(p.tiles, p.JT);
+  // Fewer items than CUs (stream: than two workgroups for each): the blocks of an item in chunks of about 32, as far as there are CUs for them.
+  // us, 1 / 2 / 4 / 8 / 16 chunks: one row behind 8192 keys 30 / 21 / 15 / 11.9 / 11.7, behind 1024 8.5 / 10.3 / ..; 256 items behind 2048 keys
+  // 12.2 / 18.0 / ..; 64 sequences up to 8192 in stream 52 / 36 / 33 / 42.
   int64_t c = (blocks + kv8_chunk_blocks / 2) / kv8_chunk_blocks;
-  if (c > kv8_cus / items) c = kv8_cus / items;
+  const int64_t room = (once ? 2 : 1) * kv8_cus / items;
+  if (c > room) c = room;
   if (c > 64) c = 64;
   p.chunks = c < 1 ? 1 : (int)c;
   p.part_floats = p.chunks > 1 ? items * p.chunks * (16 * D + 32) : 0;

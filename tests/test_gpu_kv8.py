@@ -71,9 +71,10 @@ def sees(p, key, end, mode, window, sinks):
 def plain_attention(q, k, v, n, mode, window, sinks, scale):
     """q [rows, n_q, D], k and v [n + rows, n_kv, D] in 64 bits: result, and the bound on what the kernel may be off by.
 
-    The kernel rounds the weights of the softmax to bf16 (each by at most 2^-8 of itself) and its result (2^-8 of itself); a score is a sum of D
-    products in fp32, off by at most D 2^-23 sum|q k|, which moves a weight by that times the scale, relatively.  Twice the latter,
-    for numerator and denominator, and 2^-20 for the exponentials and sums."""
+    The kernel rounds the weights w of the softmax to bf16, each by at most 2^-8 of itself, and divides by the sum of the rounded ones: the result o moves
+    by sum w_j d_j (v_j - o) / sum w_j with |d_j| <= 2^-8, at most 2^-8 (a + |o|) with a = sum w_j |v_j| / sum w_j.  Its result is rounded by 2^-8 |o| more.  A score
+    is a sum of D products in fp32, off by at most D 2^-23 sum|q k|, which moves a weight by that times the scale, relatively; twice that, for
+    numerator and denominator, and 2^-20 for the exponentials and sums."""
     rows, n_q, D = q.shape
     G = n_q // k.shape[1]
     at, key = n + np.arange(rows)[:, None], np.arange(n + rows)[None]
@@ -87,7 +88,7 @@ def plain_attention(q, k, v, n, mode, window, sinks, scale):
         moved = 2 * scale * D * 2.0 ** -23 * np.where(vis, np.abs(q[:, h]) @ np.abs(kh).T, 0).max(1, keepdims=True) + 2.0 ** -20
         a = w @ np.abs(vh)
         out[:, h] = w @ vh
-        tol[:, h] = 2.0 ** -8 * (np.abs(out[:, h]) + a) * (1 + 2.0 ** -8) + moved * (a + np.abs(out[:, h]))
+        tol[:, h] = 2.0 ** -8 * (2 * np.abs(out[:, h]) + a) * (1 + 2.0 ** -8) + moved * (a + np.abs(out[:, h]))
     return out, tol
 
 
@@ -272,8 +273,24 @@ def test_pages_past_32_bits_of_bytes():
 
 # ---- attention --------------------------------------------------------------------------------------------------------------
 
+def in_form(rig, form, n_q, M):
+    """The cache as a call that takes another form of the kernel has it, and how many times over: more (sequence, kv head, tile) items than CUs
+    (all sequences again and again, on the same pages), or page lists long enough for a cache that is not kept (nothing in their rest)."""
+    n, n_kv, D = rig.n_seq, rig.n_kv, rig.D
+    tiles = -(-M * (n_q // n_kv) // 16)
+    if form == "wide" and tiles > 1:
+        times = 256 // (n * n_kv * tiles) + 1
+        return binding.Kv8Cache(rig.codes, rig.scales, rig.pages.repeat(times, 1), rig.lens.repeat(times), rig.status), times
+    if form == "stream" and tiles == 1:
+        pages = torch.full((n, (96 << 20) // (n * n_kv * 64 * D) + 1), -1, dtype=torch.int32, device="cuda")
+        pages[:, :rig.blocks] = rig.pages
+        return binding.Kv8Cache(rig.codes, rig.scales, pages, rig.lens, rig.status), 1
+    return None, 0
+
+
 def attend(rig, q, lens, rows, mode, window=0, sinks=0, scale=0.0, workspace=None):
-    """The rows of q (per sequence [rows, n_q, D]) through the cache, which holds everything already: compared, and returned."""
+    """The rows of q (per sequence [rows, n_q, D]) through the cache, which holds everything already, in the forms that they can take: compared, and
+    returned as the plain call gives them."""
     n_q, D = q[0].shape[1:]
     M = max(1, max(rows))
     pad = torch.full((rig.n_seq, M, n_q, D), float("nan"), dtype=BF16, device="cuda")
@@ -282,20 +299,31 @@ def attend(rig, q, lens, rows, mode, window=0, sinks=0, scale=0.0, workspace=Non
     out = torch.full_like(pad, 3.5)
     rig.lens.copy_(cuda_ints(lens))
     rig.cache.bd_k_kv8_attention(pad, out, mode, window, sinks, scale, rows=cuda_ints(rows), workspace=workspace)
+    outs = [out]
+    for form in ("wide", "stream"):
+        cache, times = in_form(rig, form, n_q, M)
+        if times:
+            again = torch.full((times * rig.n_seq, M, n_q, D), 3.5, dtype=BF16, device="cuda")
+            cache.bd_k_kv8_attention(pad.repeat(times, 1, 1, 1), again, mode, window, sinks, scale, rows=cuda_ints(rows * times))
+            again = again.view(times, *pad.shape)
+            assert torch.equal(again, again[:1].expand_as(again))
+            outs.append(again[0])
     worst = 0.0
     for s in range(rig.n_seq):
-        assert (out[s, rows[s]:] == 3.5).all()
+        for o in outs:
+            assert (o[s, rows[s]:] == 3.5).all()
         if rows[s] == 0:
             continue
         end = lens[s] + rows[s]
         want, tol = plain_attention(pad[s, :rows[s]].double().cpu().numpy(), rig.plain[s].v[0, :end], rig.plain[s].v[1, :end], lens[s], mode, window, sinks,
                                     scale or D ** -0.5)
-        got = out[s, :rows[s]].double().cpu().numpy()
-        assert np.isfinite(got).all()
-        worst = max(worst, float((np.abs(got - want) / np.maximum(tol, 1e-30)).max()))
-        assert (np.abs(got - want) <= tol).all(), f"sequence {s}: {np.abs(got - want).max()} off, {worst} of the bound"
+        for o in outs:
+            got = o[s, :rows[s]].double().cpu().numpy()
+            assert np.isfinite(got).all()
+            worst = max(worst, float((np.abs(got - want) / np.maximum(tol, 1e-30)).max()))
+            assert (np.abs(got - want) <= tol).all(), f"sequence {s}: {np.abs(got - want).max()} off, {worst} of the bound"
     assert int(rig.status) == 0
-    print(f"attention: {worst:.2f} of the bound", flush=True)
+    print(f"attention: {worst:.2f} of the bound, {len(outs)} forms", flush=True)
     return out
 
 
@@ -335,6 +363,24 @@ def test_attention_on_a_long_cache(window, sinks):
     attend(rig, [random_heads(rng, 3, 8, 128), random_heads(rng, 1, 8, 128)], [40000, 9000], [3, 1], CAUSAL, window, sinks)
 
 
+@pytest.mark.parametrize("n_seq,M,n_q,n,blocks", [(64, 8, 8, 17000, 540), (14, 40, 8, 8500, 270), (512, 1, 8, 8500, 400)])
+def test_more_blocks_than_a_wavefront_looks_up_at_once(n_seq, M, n_q, n, blocks):
+    """Many sequences on the same pages, so long that every wavefront walks more than 64 blocks: one tile and eight wavefronts, two tiles and four, and one tile
+    of a cache that is not kept."""
+    rng = np.random.default_rng(n_seq)
+    D, n_kv = 64, 2 if n_seq == 64 else 1
+    rig = filled(rng, [n + M], n_kv, D)
+    pages = torch.full((n_seq, blocks), -1, dtype=torch.int32, device="cuda")
+    pages[:, :rig.blocks] = rig.pages
+    cache = binding.Kv8Cache(rig.codes, rig.scales, pages, cuda_ints([n] * n_seq), rig.status)
+    assert cache.bd_k_kv8_attention_workspace(n_q, M) == 0             # one chunk each
+    q = torch.from_numpy(random_heads(rng, M, n_q, D) * 1.5).to(BF16).cuda()[None].repeat(n_seq, 1, 1, 1)
+    out = cache.bd_k_kv8_attention(q, torch.zeros_like(q), CAUSAL)
+    want, tol = plain_attention(q[0].double().cpu().numpy(), rig.plain[0].v[0, :n + M], rig.plain[0].v[1, :n + M], n, CAUSAL, 0, 0, D ** -0.5)
+    assert (np.abs(out[0].double().cpu().numpy() - want) <= tol).all()
+    assert torch.equal(out, out[:1].expand_as(out)) and int(rig.status) == 0
+
+
 def test_scores_far_apart_and_the_scale_argument():
     """Weights that are all but one, and maxima that move late: the largest scores at the end of the cache."""
     rng = np.random.default_rng(9)
@@ -349,39 +395,45 @@ def test_scores_far_apart_and_the_scale_argument():
     attend(rig, q, [n - 4], [4], CAUSAL, 100, 3, 1.7)
 
 
-def test_what_a_row_does_not_see_does_not_reach_it():
+@pytest.mark.parametrize("rows,form", [(8, "plain"), (8, "wide"), (4, "plain"), (4, "stream")])
+def test_what_a_row_does_not_see_does_not_reach_it(rows, form):
     """NaN among keys and values: rows that see one are NaN (all of a row by a key, its dimension by a value), the others as if there were none."""
     rng = np.random.default_rng(12)
-    n, rows, D = 70, 8, 64
+    n, D, n_q = 70, 64, 4
     rig = filled(rng, [n + rows + 10], 1, D)
-    q = [random_heads(rng, rows, 4, D)]
-    clean = attend(rig, q, [n], [rows], CAUSAL)
-    nan_v = random_heads(rng, rows + 10, 1, D)
-    nan_v[5, 0, 9] = np.nan                                            # the value at position n + 5, dimension 9
-    nan_v[rows + 2:] = np.nan                                          # and all behind the last row
-    nan_k = random_heads(rng, rows + 10, 1, D)
-    nan_k[6, 0, 0] = np.nan                                            # the key at position n + 6
-    nan_k[rows + 2:] = np.nan
+    cache, times = (rig.cache, 1) if form == "plain" else in_form(rig, form, n_q, rows)
+
+    def run(q, start, *args, **kw):
+        rig.lens.fill_(start)
+        cache.lens.fill_(start)
+        q = q.repeat(times, 1, 1, 1)
+        out = cache.bd_k_kv8_attention(q, torch.zeros_like(q), CAUSAL, *args, **kw)
+        assert torch.equal(out.nan_to_num(777.0), out[:1].expand_as(out).nan_to_num(777.0))
+        return out[0]
+
+    q = torch.from_numpy(random_heads(rng, rows, n_q, D)).to(BF16).cuda()[None]
+    j, i = rows - 3, rows - 2                                          # the rows with the bad value and the bad key
+    nan_v, nan_k = random_heads(rng, rows + 10, 1, D), random_heads(rng, rows + 10, 1, D)
     good_k, good_v = nan_k.copy(), nan_v.copy()
-    good_k[6, 0, 0], good_v[5, 0, 9], good_k[rows + 2:], good_v[rows + 2:] = 0.0, 0.0, 0.0, 0.0
+    nan_v[j, 0, 9] = np.nan
+    nan_k[i, 0, 0] = np.nan
+    nan_v[rows + 2:], nan_k[rows + 2:] = np.nan, np.nan               # and all behind the last row
+    good_k[i, 0, 0], good_v[j, 0, 9], good_k[rows + 2:], good_v[rows + 2:] = 0.0, 0.0, 0.0, 0.0
     rig.write([n], [good_k], [good_v])
-    clean = attend(rig, q, [n], [rows], CAUSAL)
+    clean = run(q, n)
     rig.write([n], [nan_k], [nan_v])
-    dev = torch.from_numpy(q[0]).to(BF16).cuda()[None]
-    rig.lens.fill_(n)
-    out = rig.cache.bd_k_kv8_attention(dev, torch.zeros_like(dev), CAUSAL)
-    assert torch.equal(out[0, :5], clean[0, :5])
-    assert torch.isnan(out[0, 5, :, 9]).all() and torch.isnan(out[0, 6:]).all()
+    out = run(q, n)
+    assert torch.equal(out[:j], clean[:j])
+    assert torch.isnan(out[j, :, 9]).all() and torch.isnan(out[i:]).all()
     keep = [d for d in range(D) if d != 9]
-    assert torch.equal(out[0, 5][:, keep], clean[0, 5][:, keep])
+    assert torch.equal(out[j][:, keep], clean[j][:, keep])
     # a window that leaves them out again, and a query that is NaN itself: only its own row
-    rig.lens.fill_(n + rows)
-    rig.write([n + rows], [random_heads(rng, 4, 1, D)], [random_heads(rng, 4, 1, D)])
-    dev = torch.from_numpy(random_heads(rng, 4, 4, D)).to(BF16).cuda()[None]
-    dev[0, 2, 1] = float("nan")
-    out = rig.cache.bd_k_kv8_attention(dev, torch.zeros_like(dev), CAUSAL, window=2, sinks=10)
-    bad = torch.isnan(out[0]).any(-1)
-    assert bad[2, 1] and int(bad.sum()) == 1 and torch.isnan(out[0, 2, 1]).all()
+    rig.write([n + rows], [random_heads(rng, rows, 1, D)], [random_heads(rng, rows, 1, D)])
+    q = torch.from_numpy(random_heads(rng, rows, n_q, D)).to(BF16).cuda()[None]
+    q[0, 2, 1, 0] = float("nan")
+    out = run(q, n + rows, window=2, sinks=10)
+    bad = torch.isnan(out).any(-1)
+    assert bad[2, 1] and int(bad.sum()) == 1 and torch.isnan(out[2, 1]).all()
 
 
 def test_bad_rows_and_pages_are_reported_and_touch_nothing():
