@@ -89,7 +89,7 @@ int bd_k_trace_read(bd_ctx* ctx, unsigned long long* host_out, int capacity, int
  *   dev_status  NULL, or one int32 to which kernels OR BD_KV8_BAD_ROWS (a length or row count that is negative, more rows than M, or positions
  *               past max_blocks pages: the sequence is left out, its outputs stay as they were) and BD_KV8_BAD_PAGE (a page index outside the
  *               pool: nothing is read or written there; to the attention its keys are invisible).
- * D 64 or 128; n_pages >= 1, n_kv 1 .. 4096, n_seq 1 .. 65535, max_blocks 1 .. 2^25 and M 1 .. 2^22, else BD_E_ARG.
+ * D 64 or 128; n_kv 1 .. 4096, n_pages n_kv 1 .. 2^31, n_seq 1 .. 65535, max_blocks 1 .. 2^25 and M 1 .. 2^22, else BD_E_ARG.
  *
  * Rows.  A tensor of rows is [n_seq][M][heads][D] with heads and dimensions contiguous and the strides between sequences and
  * between rows given in elements (so a slice of a fused projection's output can be passed).  Rows are read and written 16 bytes at a

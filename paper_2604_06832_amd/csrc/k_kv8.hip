@@ -11,6 +11,7 @@ namespace {
 
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 struct Kv8Rows {          // a call's rows: their positions and how many of each sequence are real
   const int* first; const int* rows; int M;
@@ -46,6 +47,9 @@ __device__ inline void decode4(uint32_t w, float* y) {
   const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
   y[0] = a[0]; y[1] = a[1]; y[2] = b[0]; y[3] = b[1];
 }
+
+// High bit of each byte that holds a NaN.
+__device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
 template <typename T, int N> struct alignas(N * sizeof(T)) Pack { T x[N]; };
 template <typename T> __device__ inline float to_f32(T x);
@@ -138,6 +142,67 @@ __device__ inline void load_values(const uint8_t* from, uint32_t (&w)[8][2]) {
   transpose_patch(w);
 }
 
+// Largest of x over the 64 lanes, or over each half of them.
+template <bool HALVES>
+__device__ inline uint32_t lanes_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xF, 0xF, true));       // rotations inside rows of 16 lanes
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xF, 0xF, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x122, 0xF, 0xF, true));
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xF, 0xF, true));
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max((uint32_t)r[0], (uint32_t)r[1]);
+  if constexpr (HALVES) return x;
+  const auto h = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return max((uint32_t)h[0], (uint32_t)h[1]);
+}
+// Eight elements of a row as they are loaded: their largest magnitude (bits of fp32; infinities and NaN count), and their codes at scale 2^e.
+struct Row8bf16 {
+  uint4 x;
+  __device__ inline void load(const u16* p) { x = *reinterpret_cast<const uint4*>(p); }
+  __device__ inline uint32_t largest() const {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    union { uint32_t u; u16x2 h; } a{x.x & 0x7FFF7FFFu}, b{x.y & 0x7FFF7FFFu}, c{x.z & 0x7FFF7FFFu}, d{x.w & 0x7FFF7FFFu};
+    a.h = __builtin_elementwise_max(__builtin_elementwise_max(a.h, b.h), __builtin_elementwise_max(c.h, d.h));
+    return max(a.u << 16, a.u & 0xFFFF0000u);
+  }
+  __device__ inline float at(int i) const {
+    const uint32_t w = i < 2 ? x.x : i < 4 ? x.y : i < 6 ? x.z : x.w;
+    return __uint_as_float(i & 1 ? w & 0xFFFF0000u : w << 16);
+  }
+  __device__ inline uint2 codes(float scale) const { return make_uint2(pair(x.x, x.y, scale), pair(x.z, x.w, scale)); }
+  __device__ static inline uint32_t pair(uint32_t lo, uint32_t hi, float scale) {
+    union { uint32_t u; bf16x2 v; } a{lo}, b{hi};
+    union { s16x2 s; uint32_t u; } r{s16x2{0, 0}};
+    r.s = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r.s, a.v, scale, false);
+    r.s = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r.s, b.v, scale, true);
+    return r.u;
+  }
+};
+struct Row8f32 {
+  float4 x, y;
+  __device__ inline void load(const float* p) {
+    x = reinterpret_cast<const float4*>(p)[0];
+    y = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ inline float at(int i) const { return i < 4 ? (i < 2 ? (i ? x.y : x.x) : (i == 2 ? x.z : x.w)) : (i < 6 ? (i == 4 ? y.x : y.y) : (i == 6 ? y.z : y.w)); }
+  __device__ inline uint32_t largest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(at(i)) & 0x7FFFFFFFu);
+    return m;
+  }
+  __device__ inline uint2 codes(float scale) const { return make_uint2(four(x, scale), four(y, scale)); }
+  __device__ static inline uint32_t four(const float4& v, float scale) {
+    union { s16x2 s; uint32_t u; } r{s16x2{0, 0}};
+    r.s = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r.s, v.x, v.y, scale, false);
+    r.s = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r.s, v.z, v.w, scale, true);
+    return r.u;
+  }
+};
+template <typename T> struct Row8;
+template <> struct Row8<u16> : Row8bf16 {};
+template <> struct Row8<float> : Row8f32 {};
+
 template <int D, typename T>
 __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8CopyArgs a) {
   Kv8Patch<D> p;
@@ -146,19 +211,15 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8CopyArgs a) {
   const int64_t row_stride = a.row_stride[p.kv];
   const T* x = reinterpret_cast<const T*>(a.x[p.kv]) + s * a.seq_stride[p.kv] + p.h * D + p.d;
   // all loads before the first wait: the rows, then the page's word and the codes that stay
-  constexpr int N = 16 / sizeof(T);
-  Pack<T, N> raw[8][8 / N];
+  Row8<T> row[8] = {};
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int q = 0; q < 8 / N; ++q) {
-      const int t = 8 * p.g + i;
-      raw[i][q] = Pack<T, N>{};
-      if (p.on && t >= p.lo && t < p.hi) raw[i][q] = *reinterpret_cast<const Pack<T, N>*>(x + (t - p.first) * row_stride + q * N);
-    }
+  for (int i = 0; i < 8; ++i) {
+    const int t = 8 * p.g + i;
+    if (p.on && t >= p.lo && t < p.hi) row[i].load(x + (t - p.first) * row_stride);
+  }
   kv8_patch_page<D>(a, p, s);
   int e_old = kv8_e_min;
-  const bool keeps = p.on && 8 * p.g < p.lo;           // positions from before among the patch's: encoded again
+  const bool keeps = p.on && 8 * p.g < p.lo;           // positions from before among the patch's
   uint32_t old[8][2] = {};
   if (p.on && p.lo > 0) {
     e_old = kv8_byte_exponent(a.c.dev_scales[p.ph] >> (8 * p.kv));
@@ -172,55 +233,61 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8CopyArgs a) {
       load_values(p.codes + p.v_byte(), old);
     }
   }
-  float y[8][8];
   uint32_t amax = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      y[i][e] = to_f32(raw[i][e / N].x[e % N]);
-      const uint32_t u = __float_as_uint(y[i][e]) & 0x7FFFFFFFu;
-      amax = max(amax, u < 0x7F800000u ? u : 0u);                           // (finite ones; their bits order them)
-    }
-#pragma unroll
-  for (int w = D / 4; w >= 1; w >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, w, 64));
-  const int e = max(kv8_exponent(amax), e_old);
-  const float down = two_to(-e);
+  for (int i = 0; i < 8; ++i) amax = max(amax, row[i].largest());
+  amax = lanes_max<D == 64>(amax);
   uint32_t w[8][2];
-  bool nan = false;
+  int e;
+  if (__builtin_amdgcn_ballot_w64(amax >= 0x7F800000u || kv8_exponent_of(amax) > kv8_e_max) == 0ull) {
+    e = max(kv8_exponent(amax), e_old);
+    const float scale = two_to(e);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      y[i][q] *= down;
-      nan |= y[i][q] != y[i][q];
+    for (int i = 0; i < 8; ++i) {
+      const uint2 c = row[i].codes(scale);
+      w[i][0] = c.x; w[i][1] = c.y;
     }
-    w[i][0] = encode4(y[i]);
-    w[i][1] = encode4(y[i] + 4);
+  } else {                                             // infinities, NaN, or more than the largest scale holds: the finite ones decide, an element at a time
+    amax = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const uint32_t u = __float_as_uint(row[i].at(q)) & 0x7FFFFFFFu;
+        amax = max(amax, u < 0x7F800000u ? u : 0u);
+      }
+    amax = lanes_max<D == 64>(amax);
+    e = max(kv8_exponent(amax), e_old);
+    const float down = two_to(-e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float z[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) z[q] = row[i].at(4 * u + q) * down;
+        w[i][u] = encode4(z);
+      }
   }
   if (keeps) {
     const float again = two_to(max(e_old - e, -126));                       // (a smaller one would give 0 all the same)
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float z[4];
-        decode4(old[i][u], z);
-        bool bad = false;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          z[q] *= again;
-          bad |= z[q] != z[q];
-        }
+      for (int u = 0; u < 2; ++u)
         if (8 * p.g + i < p.lo) {
-          w[i][u] = encode4(z);
-          nan |= bad;
+          if (e != e_old) {
+            float z[4];
+            decode4(old[i][u], z);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) z[q] *= again;
+            w[i][u] = encode4(z);
+          } else {
+            w[i][u] = old[i][u];
+          }
         }
-      }
   }
   uint8_t* word = reinterpret_cast<uint8_t*>(a.c.dev_scales + p.ph);        // keys and values have bytes of their own
-  constexpr unsigned long long half = D == 128 ? ~0ull : 0xFFFFFFFFull;     // the lanes of one block
-  const unsigned long long nans = __builtin_amdgcn_ballot_w64(nan) >> (p.lane & (64 - D / 2));
   if (p.kv == 0) {
     const bool odd = p.lane & 1;
 #pragma unroll
@@ -233,6 +300,11 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8CopyArgs a) {
     }
     if (p.on && (p.lane & (D / 2 - 1)) == 0) word[0] = (uint8_t)(e + 127);
   } else {
+    uint32_t nan = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) nan |= nan_bytes(w[i][0]) | nan_bytes(w[i][1]);
+    const unsigned long long nans = __builtin_amdgcn_ballot_w64(nan != 0u) >> (p.lane & (64 - D / 2));
+    constexpr unsigned long long half = D == 128 ? ~0ull : 0xFFFFFFFFull;   // the lanes of one block
     transpose_patch(w);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -302,10 +374,6 @@ template <int D>
 struct Kv8Block {
   uint4 k[2][D / 64], v[D / 32];
 };
-template <int D>
-__device__ inline const uint4* kv8_codes(const bd_kv8& c, int page, int h, int lane) {
-  return reinterpret_cast<const uint4*>(c.dev_codes + ((size_t)page * c.n_kv + h) * (64 * D)) + lane;
-}
 // ONCE: they pass the caches by.
 template <bool ONCE>
 __device__ inline uint4 kv8_load(const uint4* p) {
@@ -335,8 +403,6 @@ __device__ inline bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
   o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
   return o.v;
 }
-// High bit of each byte that holds a NaN.
-__device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 __device__ inline uint32_t without_nan(uint32_t w) { return w & ~((nan_bytes(w) >> 7) * 255u); }
 
 // What a wavefront knows of the rows it works for.
@@ -350,17 +416,24 @@ __device__ inline bool kv8_visible(const Kv8Cols<JT>& w, const Kv8AttnArgs& a, i
   return kv8_sees(w.p[jt], key, w.end, a.mode, a.window, a.sinks);
 }
 
+// What a wavefront knows of a block: its number, whether every row sees all of it, whether its values hold a NaN; the scales; the lane's codes.
+constexpr uint32_t kv8_clear = 1u << 31, kv8_has_nan = 1u << 30, kv8_number = (1u << 26) - 1;
+struct Kv8Of {
+  uint32_t info;
+  float ks, vs;
+  const uint4* codes;
+};
+
 // One block of 32 keys against JT tiles of 16 columns.  S^T = K Q^T, so that a lane has eight scores of one column, and O^T = V^T P^T.
 // The running maximum follows the scores only when one exceeds it by more than 2^8: weights up to 256 lose nothing, and most
 // blocks need no maximum across lanes.  The sum of the weights is a product too, with a row of ones: what divides the result are the
 // same rounded weights that make it.  Once a block's keys are in operands the next block's are loaded over them, then likewise the values: each
-// load has the other half of a block to arrive.
+// load has the other half of a step to arrive.
 template <int D, int JT, bool ONCE>
-__device__ inline void kv8_block(Kv8Block<D>& b, uint32_t word, bool clear, const uint4* next, const bf16x8 (&qf)[JT][D / 32], f32x4 (&O)[JT][D / 16], float (&mrun)[JT],
-                                 f32x4 (&L)[JT], int kb, const Kv8Cols<JT>& cols, const Kv8AttnArgs& a, int g) {
+__device__ inline void kv8_step(Kv8Block<D>& b, const Kv8Of& of, const Kv8Of& next, const bf16x8 (&qf)[JT][D / 32], f32x4 (&O)[JT][D / 16],
+                                float (&mrun)[JT], f32x4 (&L)[JT], const Kv8Cols<JT>& cols, const Kv8AttnArgs& a, int g) {
   constexpr int DT = D / 16;
   const float c = a.c_log2;
-  const float ks = two_to(kv8_byte_exponent(word)), vs = two_to(kv8_byte_exponent(word >> 8));
   f32x4 s[JT][2];
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
@@ -368,7 +441,7 @@ __device__ inline void kv8_block(Kv8Block<D>& b, uint32_t word, bool clear, cons
     for (int jt = 0; jt < JT; ++jt) s[jt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
-      const bf16x8 k0 = widen8(b.k[t][j].x, b.k[t][j].y, ks), k1 = widen8(b.k[t][j].z, b.k[t][j].w, ks);
+      const bf16x8 k0 = widen8(b.k[t][j].x, b.k[t][j].y, of.ks), k1 = widen8(b.k[t][j].z, b.k[t][j].w, of.ks);
 #pragma unroll
       for (int jt = 0; jt < JT; ++jt) s[jt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[jt][2 * j], s[jt][t], 0, 0, 0);
 #pragma unroll
@@ -376,13 +449,14 @@ __device__ inline void kv8_block(Kv8Block<D>& b, uint32_t word, bool clear, cons
     }
   }
   __builtin_amdgcn_sched_barrier(0);                    // (the loads stay behind the last use of what they overwrite)
-  kv8_load_k<D, ONCE>(b, next);
-  if (!clear) {
+  kv8_load_k<D, ONCE>(b, next.codes);
+  if ((of.info & kv8_clear) == 0u) {
+    const int key = (int)(of.info & kv8_number) * 32 + 8 * g;
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[jt][e >> 2][e & 3] = kv8_visible<JT>(cols, a, jt, kb * 32 + 8 * g + e) ? s[jt][e >> 2][e & 3] : -INFINITY;
-    if ((word & kv8_v_nan) != 0u) {
+      for (int e = 0; e < 8; ++e) s[jt][e >> 2][e & 3] = kv8_visible<JT>(cols, a, jt, key + e) ? s[jt][e >> 2][e & 3] : -INFINITY;
+    if ((of.info & kv8_has_nan) != 0u) {
       // 0 times a NaN would reach rows that do not see it: kv8_nan_rows puts it where it belongs
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) b.v[j] = make_uint4(without_nan(b.v[j].x), without_nan(b.v[j].y), without_nan(b.v[j].z), without_nan(b.v[j].w));
@@ -421,14 +495,15 @@ __device__ inline void kv8_block(Kv8Block<D>& b, uint32_t word, bool clear, cons
   for (int jt = 0; jt < JT; ++jt) L[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, p8[jt], L[jt], 0, 0, 0);
 #pragma unroll
   for (int j = 0; j < D / 32; ++j) {
-    const bf16x8 v0 = widen8(b.v[j].x, b.v[j].y, vs), v1 = widen8(b.v[j].z, b.v[j].w, vs);
+    const bf16x8 v0 = widen8(b.v[j].x, b.v[j].y, of.vs), v1 = widen8(b.v[j].z, b.v[j].w, of.vs);
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt) O[jt][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p8[jt], O[jt][2 * j], 0, 0, 0);
 #pragma unroll
     for (int jt = 0; jt < JT; ++jt) O[jt][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p8[jt], O[jt][2 * j + 1], 0, 0, 0);
   }
   __builtin_amdgcn_sched_barrier(0);
-  kv8_load_v<D, ONCE>(b, next);
+  kv8_load_v<D, ONCE>(b, next.codes);
+  asm volatile("" ::: "memory");                        // (or they are shared with the walk for NaN and live in registers until then)
 }
 
 // A block with NaN among its values that not every row sees all of: results become NaN where a row sees one of its dimension.
@@ -470,8 +545,8 @@ __device__ inline void kv8_store(u16* o, const f32x4& a, const f32x4& b, float i
 // read the same blocks, go to one XCD (numbers that differ by multiples of 8), where its L2 serves all but the first, or are dealt to several
 // where there are fewer than 8 such units; the last groups, which see most, start first.
 template <int D, int JT, int NW> constexpr int kv8_attn_lds() { return NW * JT * ((D / 16) * 1024 + 2 * 64); }
-template <int D, int JT, int NW, int AHEAD, bool ONCE>
-__global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
+template <int D, int JT, int NW, bool ONCE>
+__global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8AttnArgs a) {
   constexpr int DT = D / 16;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   f32x4* sO = reinterpret_cast<f32x4*>(lds);                            // [NW][JT][DT][64]
@@ -492,24 +567,29 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
   if (chunk >= used) return;
   const int step = NW * used, first = wave * used + chunk;
   const int cnt = __builtin_amdgcn_readfirstlane(sp.count > first ? (sp.count - first + step - 1) / step : 0);
-  // pages and scales of the wavefront's next 64 blocks, one a lane; a block whose page lies outside the pool counts as one past the end
-  int my_page = 0, my_kb = 0;
-  uint32_t my_word = 0;
+  // what there is to know of the wavefront's next 64 blocks, one a lane; a block whose page lies outside the pool, and one past the last, is
+  // invisible to all, with the codes of page 0 for its own
+  uint32_t my_info, my_head;
+  float my_ks, my_vs;
   auto look_up = [&](int base) {
-    my_page = 0;
-    my_word = kv8_v_nan | 0x7F7F;
-    my_kb = kv8_nowhere;
+    uint32_t word = 127u | 127u << 8 | kv8_v_nan;
+    my_info = (uint32_t)kv8_nowhere | kv8_has_nan;
+    my_head = (uint32_t)h;
     if (base + lane < cnt) {
-      const int idx = first + (base + lane) * step, kb = idx < sp.sink_blocks ? idx : sp.first_block + idx - sp.sink_blocks;
-      const int page = kv8_page(a.c, s, kb);
+      const int idx = first + (base + lane) * step;
+      const bool sink = idx < sp.sink_blocks;
+      const int kb = sink ? idx : sp.first_block + idx - sp.sink_blocks, page = kv8_page(a.c, s, kb);
       if (page >= 0) {
-        my_page = page;
-        my_kb = kb;
-        my_word = a.c.dev_scales[(size_t)page * a.c.n_kv + h];
+        my_head = (uint32_t)page * (uint32_t)a.c.n_kv + (uint32_t)h;
+        word = a.c.dev_scales[my_head];
+        const bool clear = sink ? kb < sp.clear_sinks : kb >= sp.clear_lo && kb < sp.clear_hi;
+        my_info = (uint32_t)kb | (clear ? kv8_clear : 0u) | ((word & kv8_v_nan) != 0u ? kv8_has_nan : 0u);
       }
     }
+    my_ks = two_to(kv8_byte_exponent(word));
+    my_vs = two_to(kv8_byte_exponent(word >> 8));
     // waited for here: behind a branch that may have left loads open, every later wait would be one for all of them
-    asm volatile("" : "+v"(my_page), "+v"(my_kb), "+v"(my_word));
+    asm volatile("" : "+v"(my_info), "+v"(my_head), "+v"(my_ks), "+v"(my_vs));
   };
   look_up(0);
   bf16x8 qf[JT][D / 32];
@@ -532,47 +612,33 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
     L[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
     mrun[jt] = kv8_lowest;
   }
-  // AHEAD blocks are in flight, their numbers and scales with them
-  Kv8Block<D> blk[AHEAD];
-  int kbs[AHEAD];
-  uint32_t words[AHEAD];
-  auto next_of = [&](int i, int& kb, uint32_t& word) {     // (behind the last block: some page of the pool, never used)
+  auto block_of = [&](int i) {
     if ((i & 63) == 0 && i > 0) look_up(i);
-    kb = __builtin_amdgcn_readlane(my_kb, i & 63);
-    word = (uint32_t)__builtin_amdgcn_readlane((int)my_word, i & 63);
-    return kv8_codes<D>(a.c, __builtin_amdgcn_readlane(my_page, i & 63), h, lane);
+    const uint32_t head = (uint32_t)__builtin_amdgcn_readlane((int)my_head, i & 63);
+    return Kv8Of{(uint32_t)__builtin_amdgcn_readlane((int)my_info, i & 63), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), i & 63)),
+                 __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_vs), i & 63)),
+                 reinterpret_cast<const uint4*>(a.c.dev_codes + (size_t)head * (64 * D)) + lane};
   };
-  auto is_clear = [&](int kb) { return kb < sp.first_block ? kb < sp.clear_sinks : kb >= sp.clear_lo && kb < sp.clear_hi; };
   bool nan = false;
   if (cnt > 0) {
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const uint4* codes = next_of(u, kbs[u], words[u]);
-      // (in the order in which the loop will ask for them: its first wait has to hold for this entry to it too)
-      __builtin_amdgcn_sched_barrier(0);
-      kv8_load_k<D, ONCE>(blk[u], codes);
-      __builtin_amdgcn_sched_barrier(0);
-      kv8_load_v<D, ONCE>(blk[u], codes);
-    }
-    for (int i = 0; i < cnt; i += AHEAD) {
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int kb = kbs[u];          // (an odd one out is followed by one past the end: a way round it would cost every wait its count)
-        const uint32_t word = words[u];
-        const bool clear = is_clear(kb);
-        const uint4* next = next_of(i + u + AHEAD, kbs[u], words[u]);
-        kv8_block<D, JT, ONCE>(blk[u], word, clear, next, qf, O, mrun, L, kb, cols, a, g);
-        nan |= !clear && (word & kv8_v_nan) != 0u && kb != kv8_nowhere;
-      }
+    Kv8Block<D> b;
+    Kv8Of of = block_of(0);
+    kv8_load_k<D, ONCE>(b, of.codes);
+    __builtin_amdgcn_sched_barrier(0);                  // (in the order in which the loop will ask for them: its first wait has to hold for this entry to it too)
+    kv8_load_v<D, ONCE>(b, of.codes);
+    for (int i = 0; i < cnt; ++i) {
+      const Kv8Of next = block_of(i + 1);
+      kv8_step<D, JT, ONCE>(b, of, next, qf, O, mrun, L, cols, a, g);
+      nan |= (of.info & (kv8_clear | kv8_has_nan)) == kv8_has_nan && (of.info & kv8_number) != (uint32_t)kv8_nowhere;
+      of = next;
     }
   }
   if (nan) {
+    look_up(0);
     for (int i = 0; i < cnt; ++i) {
-      if (i == 0) look_up(0);
-      int kb;
-      uint32_t word;
-      const uint4* codes = next_of(i, kb, word);
-      if (!is_clear(kb) && (word & kv8_v_nan) != 0u && kb != kv8_nowhere) kv8_nan_rows<D, JT>(codes, O, kb, cols, a, g);
+      const Kv8Of of = block_of(i);
+      const int kb = (int)(of.info & kv8_number);
+      if ((of.info & (kv8_clear | kv8_has_nan)) == kv8_has_nan && kb != kv8_nowhere) kv8_nan_rows<D, JT>(of.codes, O, kb, cols, a, g);
     }
   }
 #pragma unroll
@@ -714,7 +780,7 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 int check_cache(const bd_kv8* c, int M, bool shape_only = false) {
   if (c == nullptr) return BD_E_ARG;
   if ((c->D != 64 && c->D != 128) || c->n_pages < 1 || c->n_kv < 1 || c->n_kv > 4096 || c->n_seq < 1 || c->n_seq > 65535 || c->max_blocks < 1 ||
-      c->max_blocks > (1 << 25) || M < 1 || M > kMaxRows)
+      c->max_blocks > (1 << 25) || (int64_t)c->n_pages * c->n_kv > ((int64_t)1 << 31) || M < 1 || M > kMaxRows)
     return BD_E_ARG;
   if (shape_only) return BD_OK;
   if (c->dev_codes == nullptr || !aligned16(c->dev_codes) || c->dev_scales == nullptr || c->dev_pages == nullptr) return BD_E_ARG;
@@ -744,7 +810,7 @@ int launch_copy(hipStream_t s, K kernel, const Kv8CopyArgs& a) {
   return check_launch();
 }
 
-template <int D, int JT, int NW, int AHEAD, bool ONCE>
+template <int D, int JT, int NW, bool ONCE>
 int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
   constexpr int lds = kv8_attn_lds<D, JT, NW>();
   if (lds > 65536) {
@@ -753,13 +819,13 @@ int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
     HIP_TRY(hipGetDevice(&dev));
     const uint64_t bit = (uint64_t)1 << (dev & 63);
     if (dev > 63 || (allowed.load(std::memory_order_relaxed) & bit) == 0) {
-      HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attn_kernel<D, JT, NW, AHEAD, ONCE>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+      HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attn_kernel<D, JT, NW, ONCE>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
       if (dev <= 63) allowed.fetch_or(bit, std::memory_order_relaxed);
     }
   }
   const int64_t units = (int64_t)a.c.n_seq * a.c.n_kv * p.chunks, grid = (units * p.runs + 7) / 8 * 8 * p.run_len;
   if (grid * NW * 64 >= ((int64_t)1 << 32)) return BD_E_ARG;
-  hipLaunchKernelGGL((kv8_attn_kernel<D, JT, NW, AHEAD, ONCE>), dim3((unsigned)grid), dim3(NW * 64), lds, s, a);
+  hipLaunchKernelGGL((kv8_attn_kernel<D, JT, NW, ONCE>), dim3((unsigned)grid), dim3(NW * 64), lds, s, a);
   BD_TRY(check_launch());
   if (p.chunks > 1) {
     hipLaunchKernelGGL((kv8_merge_kernel<D>), dim3((unsigned)((int64_t)a.c.n_seq * a.c.n_kv * p.tiles * (D / 32))), dim3(64), 0, s, a, JT);
@@ -770,9 +836,9 @@ int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
 template <int D>
 int launch_attn_form(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
   switch (p.form) {
-    case Kv8Form::wide: return launch_attn<D, 2, 4, 2, false>(s, a, p);
-    case Kv8Form::stream: return launch_attn<D, 1, 4, 2, true>(s, a, p);
-    default: return launch_attn<D, 1, 8, 1, false>(s, a, p);
+    case Kv8Form::wide: return launch_attn<D, 2, 4, false>(s, a, p);
+    case Kv8Form::stream: return launch_attn<D, 1, 4, true>(s, a, p);
+    default: return launch_attn<D, 1, 8, false>(s, a, p);
   }
 }
 

@@ -21,11 +21,16 @@ __host__ __device__ inline int kv8_v_byte(int tok, int d) {
   return ((d >> 5) * 4 + (tok >> 3)) * 256 + (((d >> 3) & 3) * 4 + (d & 3)) * 16 + ((d >> 2) & 1) * 8 + (tok & 7);
 }
 
-// Smallest e in [kv8_e_min, kv8_e_max] with amax <= 448 2^e; bits: those of a finite amax >= 0.  (448 = 1.75 2^8)
-__host__ __device__ inline int kv8_exponent(uint32_t bits) {
+// Smallest e >= kv8_e_min with amax <= 448 2^e; bits: those of a finite amax >= 0.  (448 = 1.75 2^8)
+__host__ __device__ inline int kv8_exponent_of(uint32_t bits) {
   const int x = (int)(bits >> 23) - 127;
   const int e = (bits & 0x7FFFFFu) <= 0x600000u ? x - 8 : x - 7;
-  return e < kv8_e_min ? kv8_e_min : e > kv8_e_max ? kv8_e_max : e;
+  return e < kv8_e_min ? kv8_e_min : e;
+}
+// The same as the cache has it, at most kv8_e_max.
+__host__ __device__ inline int kv8_exponent(uint32_t bits) {
+  const int e = kv8_exponent_of(bits);
+  return e > kv8_e_max ? kv8_e_max : e;
 }
 // The exponent that a scale word's byte stands for; bytes that no write leaves count as the nearest that one can.
 __host__ __device__ inline int kv8_byte_exponent(uint32_t byte) {
@@ -88,11 +93,11 @@ inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_bloc
     if (w < blocks) blocks = w;
   }
   // One tile and a cache too large for the last-level cache: every block has one reader and will be gone from the caches before its next use, so
-  // its loads pass them by; two blocks ahead, four wavefronts, three workgroups a CU.  us, stream and walk: 64 sequences up to 8192 (137 MB) 35.5 and
-  // 40.1, 256 up to 4096 59 and 66; 32 up to 8192 (66 MB, which stays cached between runs) 27 and 21.  Loads alone take as long as the whole kernel.
-  // More items than CUs: two tiles share each block that a wavefront loads and widens, two blocks ahead, four wavefronts, two workgroups a CU.
+  // its loads pass them by; four wavefronts, three workgroups a CU.  us, stream and walk: 64 sequences up to 8192 (137 MB) 35 and 40, 256 up to
+  // 4096 59 and 66; 32 up to 8192 (66 MB, which stays cached between runs) 27 and 21.  Loads alone take as long as the whole kernel.
+  // More items than CUs: two tiles share each block that a wavefront loads and widens; four wavefronts, two workgroups a CU.
   // Else one tile and eight wavefronts, for the shortest walk.  us, walk and wide: 256 items behind 2048 keys 13.2 and 18.1, 512 items 25.0
-  // and 19.8, 1024 rows (1024 items) behind 7168 keys 128 and 73.
+  // and 21, 1024 rows (1024 items) behind 7168 keys 128 and 81 (four tiles 105).
   const bool once = p.tiles == 1 && (int64_t)n_seq * n_kv * blocks * 64 * D >= kv8_once_bytes;
   p.form = once ? Kv8Form::stream : items > kv8_cus && p.tiles > 1 ? Kv8Form::wide : Kv8Form::walk;
   p.JT = p.form == Kv8Form::wide ? 2 : 1;
