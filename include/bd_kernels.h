@@ -89,7 +89,8 @@ int bd_k_trace_read(bd_ctx* ctx, unsigned long long* host_out, int capacity, int
  *   dev_status  NULL, or one int32 to which kernels OR BD_KV8_BAD_ROWS (a length or row count that is negative, more rows than M, or positions
  *               past max_blocks pages: the sequence is left out, its outputs stay as they were) and BD_KV8_BAD_PAGE (a page index outside the
  *               pool: nothing is read or written there; to the attention its keys are invisible).
- * D 64 or 128; n_kv 1 .. 4096, n_pages n_kv 1 .. 2^31, n_seq 1 .. 65535, max_blocks 1 .. 2^25 and M 1 .. 2^22, else BD_E_ARG.
+ * D 64 or 128; n_kv 1 .. 4096, n_pages n_kv 1 .. 2^31, n_seq 1 .. 65535, max_blocks 1 .. 2^25, M 1 .. 2^22 and M n_kv
+ * at most 2^28, else BD_E_ARG.  Outputs may not overlap what a call reads, unless it says so.
  *
  * Rows.  A tensor of rows is [n_seq][M][heads][D] with heads and dimensions contiguous and the strides between sequences and
  * between rows given in elements (so a slice of a fused projection's output can be passed).  Rows are read and written 16 bytes at a
@@ -124,7 +125,9 @@ int bd_k_kv8_read(void* hip_stream, const bd_kv8* cache, const int32_t* dev_from
  * (bd_k_kv8_write before): out = softmax(scale q k) v over the keys a row sees, to dev_out (bf16).  Row r at position p = dev_len[s] + r sees key j
  * where j < dev_len[s] + rows, and j <= p with BD_MODE_CAUSAL (any j with BD_MODE_BIDIR), and, with window > 0, where
  * p - j < window or j < sinks: the last `window` positions and the first `sinks` ones (window 0: no window, sinks is then not looked at).
- * scale > 0, or 0 for 1/sqrt(D).  Products in bf16 (codes and queries exactly, the weights of the softmax rounded to it), sums and softmax in fp32.
+ * A row that sees no key (all of its pages lie outside the pool) becomes NaN.  scale > 0, or 0 for 1/sqrt(D); n_q 1 .. 65536 and
+ * n_seq n_kv ceil(M n_q / n_kv / 16) at most 2^22.  Products in bf16 (codes and queries exactly, the weights of the softmax rounded to it), sums and softmax in
+ * fp32: scores, and values times 256 times the keys a row sees, have to stay below 2^127.
  * dev_workspace: bd_k_kv8_attention_workspace bytes (may be 0: NULL then), 16-byte aligned, free for others when the call has run;
  * calls that may overlap in time need one each.  The results do not depend on what it holds, and are the same on every run. */
 int bd_k_kv8_attention(void* hip_stream, const bd_kv8* cache, const void* dev_q, int64_t q_seq_stride, int64_t q_row_stride, int n_q, int M,
@@ -154,7 +157,8 @@ int bd_k_rope_plan(bd_rope* host_out, int D, int rotary_dim, int layout, double 
 
 /* Turns rows [n_seq][M][n_heads][D] (BD_BF16 or BD_F32; strides and alignment as above) from dev_x to dev_out, which may be dev_x itself with the same strides
  * (else the two may not overlap); dimensions from rotary_dim on are copied.  Row r of sequence s is at position dev_pos[s] + r (int32 [n_seq];
- * with M = 1 every row brings its own), dev_rows as above (a count outside 0 .. M is taken as the nearer end).  Angles in fp64, sines and products in fp32. */
+ * with M = 1 every row brings its own), dev_rows as above (a count outside 0 .. M is taken as the nearer end); n_heads 1 .. 65536, n_seq 1 .. 65535,
+ * M 1 .. 2^22.  Angles in fp64, sines and products in fp32. */
 int bd_k_rope(void* hip_stream, const bd_rope* plan, const void* dev_x, int64_t x_seq_stride, int64_t x_row_stride, void* dev_out,
               int64_t out_seq_stride, int64_t out_row_stride, int dtype, int n_heads, int n_seq, int M, const int32_t* dev_pos,
               const int32_t* dev_rows);

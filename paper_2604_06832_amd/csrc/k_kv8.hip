@@ -1,5 +1,4 @@
 // Attention on a key/value cache in 8 bits, and what fills and reads it (include/bd_kernels.h: bd_rope, bd_kv8).
-#include <atomic>
 #include <cmath>
 
 #include "kv8.h"
@@ -544,14 +543,11 @@ __device__ inline void kv8_store(u16* o, const f32x4& a, const f32x4& b, float i
 // leaves an unnormalised partial, which kv8_merge_kernel sums in the order of the chunks.  The groups of a (sequence, kv head, chunk), which
 // read the same blocks, go to one XCD (numbers that differ by multiples of 8), where its L2 serves all but the first, or are dealt to several
 // where there are fewer than 8 such units; the last groups, which see most, start first.
-template <int D, int JT, int NW> constexpr int kv8_attn_lds() { return NW * JT * ((D / 16) * 1024 + 2 * 64); }
 template <int D, int JT, int NW, bool ONCE>
 __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8AttnArgs a) {
   constexpr int DT = D / 16;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  f32x4* sO = reinterpret_cast<f32x4*>(lds);                            // [NW][JT][DT][64]
-  float* sm = reinterpret_cast<float*>(lds + NW * JT * DT * 1024);      // [NW][JT][16]
-  float* sl = sm + NW * JT * 16;
+  __shared__ f32x4 sO[NW * JT * DT * 64];                               // [NW][JT][DT][64]
+  __shared__ float sm[NW * JT * 16], sl[NW * JT * 16];                  // [NW][JT][16]
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
   const int run = (blockIdx.x / (8 * a.run_len)) * 8 + (blockIdx.x & 7), unit = run / a.runs;
   const int grp = a.groups - 1 - ((int)(blockIdx.x >> 3) % a.run_len * a.runs + run % a.runs);
@@ -726,7 +722,7 @@ template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int per) {
   __shared__ float2 s_cs[kRopeRows][64];               // (cosine, sine)
   const int s = blockIdx.y, r0 = blockIdx.x * per, tid = threadIdx.x;
-  const int rows = min(a.rows != nullptr ? a.rows[s] : a.M, a.M) - r0, n = min(rows, per);
+  const int n = min(max(min(a.rows != nullptr ? a.rows[s] : a.M, a.M), 0) - r0, per);
   if (n <= 0) return;
   const int R2 = a.plan.rotary_dim >> 1, D = a.plan.D;
   if (tid < 64 * n && (tid & 63) < R2) {
@@ -780,7 +776,8 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 int check_cache(const bd_kv8* c, int M, bool shape_only = false) {
   if (c == nullptr) return BD_E_ARG;
   if ((c->D != 64 && c->D != 128) || c->n_pages < 1 || c->n_kv < 1 || c->n_kv > 4096 || c->n_seq < 1 || c->n_seq > 65535 || c->max_blocks < 1 ||
-      c->max_blocks > (1 << 25) || (int64_t)c->n_pages * c->n_kv > ((int64_t)1 << 31) || M < 1 || M > kMaxRows)
+      c->max_blocks > (1 << 25) || (int64_t)c->n_pages * c->n_kv > ((int64_t)1 << 31) || M < 1 || M > kMaxRows ||
+      (int64_t)M * c->n_kv > (1 << 28))
     return BD_E_ARG;
   if (shape_only) return BD_OK;
   if (c->dev_codes == nullptr || !aligned16(c->dev_codes) || c->dev_scales == nullptr || c->dev_pages == nullptr) return BD_E_ARG;
@@ -804,28 +801,15 @@ int blocks_of(int M, int max_blocks) {
 
 template <typename K>
 int launch_copy(hipStream_t s, K kernel, const Kv8CopyArgs& a) {
-  const int64_t wavefronts = (int64_t)ceil_div(blocks_of(a.r.M, a.c.max_blocks), 128 / a.c.D) * 2 * a.c.n_kv;
-  if (wavefronts >= ((int64_t)1 << 26)) return BD_E_ARG;      // (2^32 threads are one too many for a launch)
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((wavefronts + 3) / 4), 1, a.c.n_seq), dim3(256), 0, s, a);
+  const int wavefronts = ceil_div(blocks_of(a.r.M, a.c.max_blocks), 128 / a.c.D) * 2 * a.c.n_kv;
+  hipLaunchKernelGGL(kernel, dim3(ceil_div(wavefronts, 4), 1, a.c.n_seq), dim3(256), 0, s, a);
   return check_launch();
 }
 
 template <int D, int JT, int NW, bool ONCE>
 int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
-  constexpr int lds = kv8_attn_lds<D, JT, NW>();
-  if (lds > 65536) {
-    static std::atomic<uint64_t> allowed{0};              // devices on which this kernel may have so much LDS already
-    int dev = 0;
-    HIP_TRY(hipGetDevice(&dev));
-    const uint64_t bit = (uint64_t)1 << (dev & 63);
-    if (dev > 63 || (allowed.load(std::memory_order_relaxed) & bit) == 0) {
-      HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_attn_kernel<D, JT, NW, ONCE>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-      if (dev <= 63) allowed.fetch_or(bit, std::memory_order_relaxed);
-    }
-  }
   const int64_t units = (int64_t)a.c.n_seq * a.c.n_kv * p.chunks, grid = (units * p.runs + 7) / 8 * 8 * p.run_len;
-  if (grid * NW * 64 >= ((int64_t)1 << 32)) return BD_E_ARG;
-  hipLaunchKernelGGL((kv8_attn_kernel<D, JT, NW, ONCE>), dim3((unsigned)grid), dim3(NW * 64), lds, s, a);
+  hipLaunchKernelGGL((kv8_attn_kernel<D, JT, NW, ONCE>), dim3((unsigned)grid), dim3(NW * 64), 0, s, a);
   BD_TRY(check_launch());
   if (p.chunks > 1) {
     hipLaunchKernelGGL((kv8_merge_kernel<D>), dim3((unsigned)((int64_t)a.c.n_seq * a.c.n_kv * p.tiles * (D / 32))), dim3(64), 0, s, a, JT);
@@ -845,6 +829,7 @@ int launch_attn_form(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
 int check_attn(const bd_kv8* c, int n_q, int M, int window, int sinks, bool shape_only, Kv8Plan* p) {
   BD_TRY(check_cache(c, M, shape_only));
   if (n_q < 1 || n_q > (1 << 16) || n_q % c->n_kv != 0 || window < 0 || sinks < 0) return BD_E_ARG;
+  if (kv8_items(c->n_seq, M, n_q, c->n_kv) > ((int64_t)1 << 22)) return BD_E_ARG;      // (a launch has less than 2^32 threads)
   *p = kv8_plan(c->n_seq, M, n_q, c->n_kv, c->D, c->max_blocks, window, sinks);
   return BD_OK;
 }

@@ -83,10 +83,11 @@ struct Kv8Plan {
 };
 constexpr int kv8_chunk_blocks = 32, kv8_cus = 256;
 constexpr int64_t kv8_once_bytes = (int64_t)96 << 20;
+inline int64_t kv8_items(int n_seq, int M, int n_q, int n_kv) { return (int64_t)n_seq * n_kv * (((int64_t)M * (n_q / n_kv) + 15) / 16); }
 inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_blocks, int window, int sinks) {
   Kv8Plan p{};
   p.tiles = (int)(((int64_t)M * (n_q / n_kv) + 15) / 16);
-  const int64_t items = (int64_t)n_seq * n_kv * p.tiles;
+  const int64_t items = kv8_items(n_seq, M, n_q, n_kv);
   int64_t blocks = max_blocks;
   if (window > 0) {
     const int64_t w = ((int64_t)window + M + 62) / 32 + 1 + ((int64_t)sinks + 31) / 32;

@@ -154,6 +154,14 @@ static void refusals() {
   for (int v : {0, -4, 5, 1 << 17}) { n_q = v; CHECK(attn(&c) == BD_E_ARG); } n_q = 4;
   for (int v : {0, (1 << 22) + 1}) { M = v; CHECK(attn(&c) == BD_E_ARG); } M = 4;
   for (float v : {-1.f, std::numeric_limits<float>::quiet_NaN(), std::numeric_limits<float>::infinity()}) { scale = v; CHECK(attn(&c) == BD_E_ARG); } scale = 0.f;
+  M = 1 << 22; n_q = 8; CHECK(attn(&c) == BD_E_ARG); M = 4; n_q = 4;       // more tiles than a launch has room for
+  {
+    bd_kv8 many = c;
+    many.n_kv = 4096;
+    CHECK(write(&many, mem, 1 << 20, 1 << 20, BD_BF16, (1 << 16) + 1) == BD_E_ARG);
+    many.n_pages = 1 << 20;
+    CHECK(write(&many, mem, 1 << 20, 1 << 20) == BD_E_ARG);
+  }
   q_row = 252; CHECK(attn(&c) == BD_E_ARG); q_row = 256;
   o_row = 248; CHECK(attn(&c) == BD_E_ARG); o_row = 256;
   q = nullptr; CHECK(attn(&c) == BD_E_ARG); q = mem;

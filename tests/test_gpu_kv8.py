@@ -250,6 +250,18 @@ def test_read_from_the_middle(M):
     assert (k[1, rows[1]:] == 7.25).all()
 
 
+def test_a_new_cache_holds_zeros_until_it_is_written():
+    pages = cuda_ints([[2, 0], [1, 3]])
+    cache = binding.Kv8Cache.empty(4, 2, 64, pages, cuda_ints([0, 0]))
+    k, v = torch.full((2, 2, 40, 2, 64), 7.25, device="cuda")
+    cache.bd_k_kv8_read(None, k, v)
+    assert (k == 0).all() and (v == 0).all()
+    x = torch.randint(-8, 9, (2, 40, 2, 64), device="cuda").float()    # (integers to 8 are e4m3 numbers)
+    cache.bd_k_kv8_write(x, -x)
+    cache.bd_k_kv8_read(None, k, v)
+    assert torch.equal(k, x) and torch.equal(v, -x)
+
+
 def test_pages_past_32_bits_of_bytes():
     n_pages, n_kv, D = 300000, 2, 128                                  # 4.9 GB of codes
     codes = torch.zeros((n_pages, n_kv, 64 * D), dtype=torch.uint8, device="cuda")
@@ -570,6 +582,16 @@ def test_rope_with_a_position_for_each_row():
         src = x[i].double().cpu().numpy()
         want = plain_rope(src, p, plan)
         assert (np.abs(got[i].double().cpu().numpy() - want) <= rope_tolerance(want, src, BF16, 1.0)).all()
+
+
+def test_rope_takes_counts_outside_the_rows_as_the_nearer_end():
+    plan = binding.bd_k_rope_plan(64)
+    x = torch.randn((4, 1100, 2, 64), device="cuda").to(BF16)          # (4400 rows: several of a sequence to a workgroup)
+    pos = cuda_ints([0, 5, 9, 1])
+    out = torch.full_like(x, 7.25)
+    binding.bd_k_rope(plan, x, pos, out=out, rows=cuda_ints([-2 ** 31, -1, 2 ** 31 - 1, 1101]))
+    whole = binding.bd_k_rope(plan, x, pos)
+    assert (out[:2] == 7.25).all() and torch.equal(out[2:], whole[2:])
 
 
 # ---- together -------------------------------------------------------------------------------------------------------------------
