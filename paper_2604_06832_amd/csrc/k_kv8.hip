@@ -18,19 +18,25 @@ struct Kv8Rows {          // a call's rows: their positions and how many of each
 
 // First position and number of rows of sequence s; false (and reported) where they make no sense.
 __device__ inline bool kv8_take(const bd_kv8& c, const Kv8Rows& r, int s, int& first, int& rows) {
-  first = r.first != nullptr ? r.first[s] : 0;
-  rows = r.rows != nullptr ? r.rows[s] : r.M;
+  first = 0;
+  rows = r.M;
+  if (r.first != nullptr || r.rows != nullptr) {       // (both loads before a wait)
+    const int x = (r.first != nullptr ? r.first : r.rows)[s], y = (r.rows != nullptr ? r.rows : r.first)[s];
+    if (r.first != nullptr) first = x;
+    if (r.rows != nullptr) rows = y;
+  }
   if (kv8_rows_ok(first, rows, r.M, c.max_blocks)) return true;
   if (c.dev_status != nullptr && threadIdx.x == 0) atomicOr(c.dev_status, BD_KV8_BAD_ROWS);
   return false;
 }
-// Page of block kb of sequence s; -1 (and reported) where it lies outside the pool.
-__device__ inline int kv8_page(const bd_kv8& c, int s, int kb) {
-  const int page = c.dev_pages[(size_t)s * c.max_blocks + kb];
+// The page, or -1 (and reported) where it lies outside the pool.
+__device__ inline int kv8_in_pool(const bd_kv8& c, int page) {
   if ((unsigned)page < (unsigned)c.n_pages) return page;
   if (c.dev_status != nullptr) atomicOr(c.dev_status, BD_KV8_BAD_PAGE);
   return -1;
 }
+// Page of block kb of sequence s.
+__device__ inline int kv8_page(const bd_kv8& c, int s, int kb) { return kv8_in_pool(c, c.dev_pages[(size_t)s * c.max_blocks + kb]); }
 
 __device__ inline float two_to(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
@@ -72,6 +78,7 @@ struct Kv8CopyArgs {
   Kv8Rows r;
   void* x[2];                                          // keys, values
   int64_t seq_stride[2], row_stride[2];
+  Kv8Div by_heads;                                     // divisions by 2 n_kv
 };
 
 template <int D>
@@ -90,7 +97,7 @@ __device__ inline bool kv8_patch(const Kv8CopyArgs& a, Kv8Patch<D>& p, int& s) {
   constexpr int per = D / 8, U = 128 / D;              // lanes of a row, blocks of a wavefront
   p.lane = threadIdx.x & 63;
   const int u = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int hk = u % (2 * a.c.n_kv);
+  const int pair = kv8_quotient(u, a.by_heads), hk = u - pair * 2 * a.c.n_kv;
   p.h = hk >> 1;
   p.kv = hk & 1;
   p.g = (p.lane / per) & 3;
@@ -98,7 +105,7 @@ __device__ inline bool kv8_patch(const Kv8CopyArgs& a, Kv8Patch<D>& p, int& s) {
   s = blockIdx.z;
   int n, rows;
   if (!kv8_take(a.c, a.r, s, n, rows)) return false;
-  const int kb = n / 32 + (u / (2 * a.c.n_kv)) * U + p.lane / (4 * per);
+  const int kb = n / 32 + pair * U + p.lane / (4 * per);
   p.first = n - kb * 32;
   p.lo = max(p.first, 0);
   p.hi = (int)min((int64_t)n + rows - (int64_t)kb * 32, (int64_t)32);
@@ -363,7 +370,8 @@ struct Kv8AttnArgs {
   float* part;
   int n_q, mode, window, sinks;
   float c_log2;                 // scale * log2(e)
-  int tiles, groups, chunks, runs, run_len;
+  int tiles, groups, chunks, runs, run_len, G;
+  Kv8Div by_len, by_runs, by_chunks, by_kv, by_G;      // divisions by run_len, runs, chunks, n_kv, G
 };
 constexpr int kv8_nowhere = 1 << 25;      // number of a block that is none: past every sequence's end
 constexpr float kv8_lowest = -3.0e38f;   // start of a running maximum: below every finite score, and finite itself
@@ -549,20 +557,27 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
   __shared__ f32x4 sO[NW * JT * DT * 64];                               // [NW][JT][DT][64]
   __shared__ float sm[NW * JT * 16], sl[NW * JT * 16];                  // [NW][JT][16]
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-  const int run = (blockIdx.x / (8 * a.run_len)) * 8 + (blockIdx.x & 7), unit = run / a.runs;
-  const int grp = a.groups - 1 - ((int)(blockIdx.x >> 3) % a.run_len * a.runs + run % a.runs);
+  // (all arguments with one wait)
+  asm volatile("" ::"s"(a.c.dev_codes), "s"(a.c.dev_scales), "s"(a.c.dev_pages), "s"(a.c.max_blocks), "s"(a.r.first), "s"(a.q), "s"(a.q_row), "s"(a.window),
+               "s"(a.c_log2), "s"(a.tiles), "s"(a.by_runs.mul), "s"(a.by_G.mul));
+  const int eighth = blockIdx.x >> 3, turn = kv8_quotient(eighth, a.by_len), run = turn * 8 + (blockIdx.x & 7), unit = kv8_quotient(run, a.by_runs);
+  const int grp = a.groups - 1 - ((eighth - turn * a.run_len) * a.runs + run - unit * a.runs);
   if (grp < 0 || unit >= a.c.n_seq * a.c.n_kv * a.chunks) return;
-  const int chunk = unit % a.chunks, h = (unit / a.chunks) % a.c.n_kv, s = unit / (a.chunks * a.c.n_kv);
+  const int sh = kv8_quotient(unit, a.by_chunks), chunk = unit - sh * a.chunks, s = kv8_quotient(sh, a.by_kv), h = sh - s * a.c.n_kv;
+  // without a window and chunks the wavefront's first blocks are known before the length is: their pages are asked for at the same time
+  const bool from_0 = a.window == 0 && a.chunks == 1;
+  int early = a.c.dev_pages[(size_t)s * a.c.max_blocks + min(wave + lane * NW, a.c.max_blocks - 1)];
   int n, rows;
   if (!kv8_take(a.c, a.r, s, n, rows)) return;
-  const int G = a.n_q / a.c.n_kv, ncols = rows * G, c0 = grp * JT * 16;
+  const int G = a.G, ncols = rows * G, c0 = grp * JT * 16;
   if (c0 >= ncols) return;
-  const int r0 = c0 / G, r1 = (min(c0 + JT * 16, ncols) - 1) / G;
+  const int r0 = kv8_quotient(c0, a.by_G), r1 = kv8_quotient(min(c0 + JT * 16, ncols) - 1, a.by_G);
   const Kv8Span sp = kv8_span(n, rows, r0, r1, a.mode, a.window, a.sinks);
   const int used = kv8_chunks_used(sp.count, a.chunks);
   if (chunk >= used) return;
   const int step = NW * used, first = wave * used + chunk;
-  const int cnt = __builtin_amdgcn_readfirstlane(sp.count > first ? (sp.count - first + step - 1) / step : 0);
+  const int left = (sp.count - first + step - 1);
+  const int cnt = __builtin_amdgcn_readfirstlane(sp.count <= first ? 0 : used == 1 ? left / NW : left / step);
   // what there is to know of the wavefront's next 64 blocks, one a lane; a block whose page lies outside the pool, and one past the last, is
   // invisible to all, with the codes of page 0 for its own
   uint32_t my_info, my_head;
@@ -574,7 +589,8 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
     if (base + lane < cnt) {
       const int idx = first + (base + lane) * step;
       const bool sink = idx < sp.sink_blocks;
-      const int kb = sink ? idx : sp.first_block + idx - sp.sink_blocks, page = kv8_page(a.c, s, kb);
+      const int kb = sink ? idx : sp.first_block + idx - sp.sink_blocks;
+      const int page = kv8_in_pool(a.c, base == 0 && from_0 ? early : a.c.dev_pages[(size_t)s * a.c.max_blocks + kb]);
       if (page >= 0) {
         my_head = (uint32_t)page * (uint32_t)a.c.n_kv + (uint32_t)h;
         word = a.c.dev_scales[my_head];
@@ -596,8 +612,9 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
 #pragma unroll
   for (int jt = 0; jt < JT; ++jt) {
     const int cc = min(c0 + jt * 16 + col, ncols - 1);                   // (columns past the last one repeat it and store nothing)
-    cols.p[jt] = n + cc / G;
-    const u16* qp = a.q + s * a.q_seq + (cc / G) * a.q_row + (h * G + cc % G) * D + 16 * g;
+    const int r = kv8_quotient(cc, a.by_G);
+    cols.p[jt] = n + r;
+    const u16* qp = a.q + s * a.q_seq + r * a.q_row + (h * G + cc - r * G) * D + 16 * g;
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
       qf[jt][2 * j] = *reinterpret_cast<const bf16x8*>(qp + 64 * j);
@@ -649,7 +666,7 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
   __syncthreads();
   // the wavefronts share out the pairs of d-tiles
   for (int item = wave; item < JT * (DT / 2); item += NW) {
-    const int jt = item / (DT / 2), j = item % (DT / 2), cc = c0 + jt * 16 + col;
+    const int jt = item / (DT / 2), j = item % (DT / 2), cc = c0 + jt * 16 + col, r = kv8_quotient(cc, a.by_G);
     float m = kv8_lowest, f[NW], l = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) m = fmaxf(m, sm[(w * JT + jt) * 16 + col]);
@@ -662,7 +679,7 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
       o1 += sO[((w * JT + jt) * DT + 2 * j + 1) * 64 + lane] * f[w];
     }
     if (used == 1) {
-      if (cc < ncols) kv8_store(a.out + s * a.o_seq + (cc / G) * a.o_row + (h * G + cc % G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
+      if (cc < ncols) kv8_store(a.out + s * a.o_seq + r * a.o_row + (h * G + cc - r * G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
     } else if (c0 + jt * 16 < ncols) {
       float* pp = a.part + ((((int64_t)s * a.c.n_kv + h) * a.tiles + grp * JT + jt) * a.chunks + chunk) * (16 * D + 32);
       *reinterpret_cast<f32x4*>(pp + (2 * j * 64 + lane) * 4) = o0;
@@ -675,34 +692,60 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
   }
 }
 
-// The chunks of a tile summed in their order: one wavefront per (sequence, kv head, tile, pair of d-tiles).
+// The chunks of a tile summed in their order: one wavefront per (sequence, kv head, tile, pair of d-tiles).  All it does is to wait for memory, so
+// the first eight partials are asked for before it is known how many there are (those that no group left are not looked at).
 template <int D>
 __global__ __launch_bounds__(64) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
+  constexpr int P = 8, size = 16 * D + 32;
   const int lane = threadIdx.x, col = lane & 15, g = lane >> 4;
-  const int j = blockIdx.x % (D / 32), tile = (blockIdx.x / (D / 32)) % a.tiles, sh = blockIdx.x / (D / 32 * a.tiles);
-  const int h = sh % a.c.n_kv, s = sh / a.c.n_kv;
+  const int j = blockIdx.x % (D / 32), item = blockIdx.x / (D / 32), sh = item / a.tiles, tile = item - sh * a.tiles;
+  const int s = kv8_quotient(sh, a.by_kv), h = sh - s * a.c.n_kv;
+  const float* base = a.part + (int64_t)item * a.chunks * size;
+  float pm[P], pl[P];
+  f32x4 p0[P], p1[P];
+  auto ask = [&](int from) {
+#pragma unroll
+    for (int c = 0; c < P; ++c) {
+      const float* pp = base + min(from + c, a.chunks - 1) * size;
+      pm[c] = pp[16 * D + col];
+      pl[c] = pp[16 * D + 16 + col];
+      p0[c] = *reinterpret_cast<const f32x4*>(pp + (2 * j * 64 + lane) * 4);
+      p1[c] = *reinterpret_cast<const f32x4*>(pp + ((2 * j + 1) * 64 + lane) * 4);
+    }
+  };
+  ask(0);
   int n, rows;
   if (!kv8_take(a.c, a.r, s, n, rows)) return;
-  const int G = a.n_q / a.c.n_kv, ncols = rows * G, c0 = tile / JT * JT * 16, cc = tile * 16 + col;
+  const int G = a.G, ncols = rows * G, c0 = tile / JT * JT * 16, cc = tile * 16 + col;
   if (tile * 16 >= ncols) return;
-  const Kv8Span sp = kv8_span(n, rows, c0 / G, (min(c0 + JT * 16, ncols) - 1) / G, a.mode, a.window, a.sinks);
+  const Kv8Span sp = kv8_span(n, rows, kv8_quotient(c0, a.by_G), kv8_quotient(min(c0 + JT * 16, ncols) - 1, a.by_G), a.mode, a.window, a.sinks);
   const int used = kv8_chunks_used(sp.count, a.chunks);
   if (used == 1) return;
-  const float* base = a.part + ((int64_t)sh * a.tiles + tile) * a.chunks * (16 * D + 32);
-  float m = kv8_lowest;
-#pragma unroll 8
-  for (int c = 0; c < used; ++c) m = fmaxf(m, base[c * (16 * D + 32) + 16 * D + col]);
-  float l = 0.f;
+  float m = kv8_lowest, l = 0.f;
   f32x4 o0 = f32x4{0.f, 0.f, 0.f, 0.f}, o1 = o0;
-#pragma unroll 4
-  for (int c = 0; c < used; ++c) {
-    const float* pp = base + c * (16 * D + 32);
-    const float f = __builtin_amdgcn_exp2f(pp[16 * D + col] - m);
-    l += pp[16 * D + 16 + col] * f;
-    o0 += *reinterpret_cast<const f32x4*>(pp + (2 * j * 64 + lane) * 4) * f;
-    o1 += *reinterpret_cast<const f32x4*>(pp + ((2 * j + 1) * 64 + lane) * 4) * f;
+  for (int from = 0;;) {
+    float top = m;
+#pragma unroll
+    for (int c = 0; c < P; ++c) top = from + c < used ? fmaxf(top, pm[c]) : top;
+    const float again = __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    l *= again;
+    o0 *= again;
+    o1 *= again;
+#pragma unroll
+    for (int c = 0; c < P; ++c)
+      if (from + c < used) {
+        const float f = __builtin_amdgcn_exp2f(pm[c] - m);
+        l += pl[c] * f;
+        o0 += p0[c] * f;
+        o1 += p1[c] * f;
+      }
+    from += P;
+    if (from >= used) break;
+    ask(from);
   }
-  if (cc < ncols) kv8_store(a.out + s * a.o_seq + (cc / G) * a.o_row + (h * G + cc % G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
+  const int r = kv8_quotient(cc, a.by_G);
+  if (cc < ncols) kv8_store(a.out + s * a.o_seq + r * a.o_row + (h * G + cc - r * G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
 }
 
 // ---- rotary positions -----------------------------------------------------------------------------------------------------
@@ -712,12 +755,14 @@ struct RopeArgs {
   int64_t x_seq, x_row, y_seq, y_row;
   const int* pos; const int* rows;
   int heads, M;
+  Kv8Div by_items;                                     // divisions by the items of a row
 };
 
 // A workgroup takes `per` rows: sines and cosines of their angles once for all heads (fp64 up to the reduced angle: at position 2^20 an
 // angle in fp32 is off by up to 2^-5), then the heads.  Bound by the rows' bytes: 16 a lane and access, VEC, where the two halves of a rotary part
 // fall on 16 bytes (with neighbouring pairs always), else an element at a time.
 constexpr int kRopeRows = 4;
+__host__ __device__ inline int rope_item_log(int D, int N) { return (D == 128 ? 6 : 5) - (N == 8 ? 3 : N == 4 ? 2 : 0); }
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int per) {
   __shared__ float2 s_cs[kRopeRows][64];               // (cosine, sine)
@@ -738,9 +783,9 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int per) {
   constexpr int N = VEC ? 16 / sizeof(T) : 1;
   typedef Pack<T, N> V;
   // an item: two vectors of a head whose elements make pairs (half), or that lie side by side (neighbouring pairs and the rest of the head)
-  const int item_log = (D == 128 ? 6 : 5) - (N == 8 ? 3 : N == 4 ? 2 : 0), items = a.heads << item_log;
+  const int item_log = rope_item_log(D, N), items = a.heads << item_log;
   for (int i = tid; i < n * items; i += 256) {
-    const int r = i / items, k = i % items, h = k >> item_log, j = k & ((1 << item_log) - 1);
+    const int r = kv8_quotient(i, a.by_items), k = i - r * items, h = k >> item_log, j = k & ((1 << item_log) - 1);
     const bool turn = j * N < R2;
     if (in_place && !turn) continue;
     const int d0 = h * D + (half && turn ? j * N : 2 * j * N), d1 = half && turn ? d0 + R2 : d0 + N;
@@ -846,7 +891,7 @@ extern "C" int bd_k_kv8_write(void* hip_stream, const bd_kv8* cache, const void*
   BD_TRY(check_rows(dev_v, dtype, v_seq_stride, v_row_stride, cache->n_seq, M));
   if (cache->dev_len == nullptr) return BD_E_ARG;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const Kv8CopyArgs a{*cache, {cache->dev_len, dev_rows, M}, {const_cast<void*>(dev_k), const_cast<void*>(dev_v)}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}};
+  const Kv8CopyArgs a{*cache, {cache->dev_len, dev_rows, M}, {const_cast<void*>(dev_k), const_cast<void*>(dev_v)}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}, kv8_div(2 * cache->n_kv)};
   if (cache->D == 128) return dtype == BD_F32 ? launch_copy(s, kv8_write_kernel<128, float>, a) : launch_copy(s, kv8_write_kernel<128, u16>, a);
   return dtype == BD_F32 ? launch_copy(s, kv8_write_kernel<64, float>, a) : launch_copy(s, kv8_write_kernel<64, u16>, a);
 }
@@ -859,7 +904,7 @@ extern "C" int bd_k_kv8_read(void* hip_stream, const bd_kv8* cache, const int32_
   BD_TRY(check_rows(dev_k_out, dtype, k_seq_stride, k_row_stride, cache->n_seq, M, least));
   BD_TRY(check_rows(dev_v_out, dtype, v_seq_stride, v_row_stride, cache->n_seq, M, least));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const Kv8CopyArgs a{*cache, {dev_from, dev_rows, M}, {dev_k_out, dev_v_out}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}};
+  const Kv8CopyArgs a{*cache, {dev_from, dev_rows, M}, {dev_k_out, dev_v_out}, {k_seq_stride, v_seq_stride}, {k_row_stride, v_row_stride}, kv8_div(2 * cache->n_kv)};
   if (cache->D == 128) return dtype == BD_F32 ? launch_copy(s, kv8_read_kernel<128, float>, a) : launch_copy(s, kv8_read_kernel<128, u16>, a);
   return dtype == BD_F32 ? launch_copy(s, kv8_read_kernel<64, float>, a) : launch_copy(s, kv8_read_kernel<64, u16>, a);
 }
@@ -891,7 +936,8 @@ extern "C" int bd_k_kv8_attention(void* hip_stream, const bd_kv8* cache, const v
   a.part = static_cast<float*>(dev_workspace);
   a.n_q = n_q; a.mode = mode; a.window = window; a.sinks = sinks;
   a.c_log2 = (scale > 0.f ? scale : 1.f / std::sqrt((float)cache->D)) * 1.4426950408889634f;
-  a.tiles = p.tiles; a.groups = p.groups; a.chunks = p.chunks; a.runs = p.runs; a.run_len = p.run_len;
+  a.tiles = p.tiles; a.groups = p.groups; a.chunks = p.chunks; a.runs = p.runs; a.run_len = p.run_len; a.G = n_q / cache->n_kv;
+  a.by_len = kv8_div(p.run_len); a.by_runs = kv8_div(p.runs); a.by_chunks = kv8_div(p.chunks); a.by_kv = kv8_div(cache->n_kv); a.by_G = kv8_div(a.G);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (cache->D == 128) return launch_attn_form<128>(s, a, p);
   return launch_attn_form<64>(s, a, p);
@@ -942,6 +988,7 @@ extern "C" int bd_k_rope(void* hip_stream, const bd_rope* plan, const void* dev_
   const int N = dtype == BD_F32 ? 4 : 8;
   const bool vec = plan->layout == BD_ROPE_INTERLEAVED || plan->rotary_dim % (2 * N) == 0;
   const int per = (int64_t)M * n_seq >= 4096 ? kRopeRows : 1;               // few rows: a workgroup each
+  a.by_items = kv8_div(n_heads << rope_item_log(plan->D, vec ? N : 1));
   const dim3 grid(ceil_div(M, per), n_seq);
   if (dtype == BD_F32) {
     if (vec) hipLaunchKernelGGL((rope_kernel<float, true>), grid, dim3(256), 0, s, a, per);

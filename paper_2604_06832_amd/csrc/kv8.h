@@ -44,6 +44,19 @@ __host__ __device__ inline bool kv8_rows_ok(int first, int rows, int M, int max_
   return first >= 0 && rows >= 0 && rows <= M && (int64_t)first + rows <= (int64_t)max_blocks * BD_KV8_PAGE;
 }
 
+// Division of 0 <= x < 2^31 by the same d >= 1 every time: x/d = (floor(x mul / 2^32) + x) / 2^shift with 2^shift >= d > 2^(shift - 1) and
+// mul = floor(2^32 (2^shift - d) / d) + 1 (mul + 2^32 exceeds 2^(32 + shift)/d by at most 1, too little to reach the next quotient).
+struct Kv8Div { uint32_t mul, shift; };
+inline Kv8Div kv8_div(int d) {
+  Kv8Div v{0, 0};
+  while (((int64_t)1 << v.shift) < d) ++v.shift;
+  v.mul = (uint32_t)(((((uint64_t)1 << v.shift) - (uint64_t)d) << 32) / (uint64_t)d + 1);
+  return v;
+}
+__host__ __device__ inline int kv8_quotient(int x, Kv8Div d) {
+  return (int)(((uint32_t)(((uint64_t)(uint32_t)x * d.mul) >> 32) + (uint32_t)x) >> d.shift);
+}
+
 // What rows r0 .. r1 (positions n + r0 .. n + r1) of a sequence with `rows` rows can see: the blocks of the first `sinks`
 // positions, then those from the window's start to the last visible key: block number idx of `count` is idx for
 // idx < sink_blocks, and first_block + idx - sink_blocks from there.  [clear_lo, clear_hi): blocks from the window all of whose keys every

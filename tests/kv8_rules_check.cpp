@@ -48,6 +48,22 @@ static void exponents() {
   CHECK(kv8_byte_exponent(0x300u | (127 + 5)) == 5);
 }
 
+static void quotients() {
+  const int big = std::numeric_limits<int>::max();
+  std::vector<int> ds;
+  for (int d = 1; d <= 4100; ++d) ds.push_back(d);
+  for (int b = 13; b < 31; ++b)
+    for (int o : {-1, 0, 1}) ds.push_back((1 << b) + o);
+  for (int d : {big - 1, big, 1000003, 65536 * 64}) ds.push_back(d);
+  for (int d : ds) {
+    const Kv8Div v = kv8_div(d);
+    auto at = [&](int64_t x) { if (x >= 0 && x <= big) CHECK(kv8_quotient((int)x, v) == (int)x / d); };
+    for (int64_t k : {0, 1, 2, 3, 7, 100, 4095, 65537, big / d - 1, big / d})
+      for (int o : {-1, 0, 1}) at(k * d + o);               // (an int64: past the range it is left out)
+    for (int x : {0, 1, big - 1, big}) at(x);
+  }
+}
+
 static void rows() {
   const int big = std::numeric_limits<int>::max();
   CHECK(kv8_rows_ok(0, 0, 1, 1) && kv8_rows_ok(0, 32, 32, 1) && kv8_rows_ok(32, 0, 4, 1) && kv8_rows_ok(31, 1, 4, 1));
@@ -198,6 +214,7 @@ static void refusals() {
 int main() {
   layout();
   exponents();
+  quotients();
   rows();
   span();
   plan();
