@@ -694,10 +694,10 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
 
 // The chunks of a tile summed in their order: one wavefront per (sequence, kv head, tile, pair of d-tiles).  All it does is to wait for memory, so
 // the first eight partials are asked for before it is known how many there are (those that no group left are not looked at).
-template <int D>
-__global__ __launch_bounds__(64) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
+template <int D, int W>
+__global__ __launch_bounds__(64 * W) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
   constexpr int P = 8, size = 16 * D + 32;
-  const int lane = threadIdx.x, col = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
   const int j = blockIdx.x % (D / 32), item = blockIdx.x / (D / 32), sh = item / a.tiles, tile = item - sh * a.tiles;
   const int s = kv8_quotient(sh, a.by_kv), h = sh - s * a.c.n_kv;
   const float* base = a.part + (int64_t)item * a.chunks * size;
@@ -713,7 +713,7 @@ __global__ __launch_bounds__(64) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
       p1[c] = *reinterpret_cast<const f32x4*>(pp + ((2 * j + 1) * 64 + lane) * 4);
     }
   };
-  ask(0);
+  ask(wave * P);
   int n, rows;
   if (!kv8_take(a.c, a.r, s, n, rows)) return;
   const int G = a.G, ncols = rows * G, c0 = tile / JT * JT * 16, cc = tile * 16 + col;
@@ -723,7 +723,7 @@ __global__ __launch_bounds__(64) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
   if (used == 1) return;
   float m = kv8_lowest, l = 0.f;
   f32x4 o0 = f32x4{0.f, 0.f, 0.f, 0.f}, o1 = o0;
-  for (int from = 0;;) {
+  for (int from = wave * P;;) {
     float top = m;
 #pragma unroll
     for (int c = 0; c < P; ++c) top = from + c < used ? fmaxf(top, pm[c]) : top;
@@ -740,9 +740,29 @@ __global__ __launch_bounds__(64) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
         o0 += p0[c] * f;
         o1 += p1[c] * f;
       }
-    from += P;
+    from += W * P;
     if (from >= used) break;
     ask(from);
+  }
+  if constexpr (W > 1) {
+    __shared__ f32x4 so[W][2][64];
+    __shared__ float2 sml[W][16];
+    so[wave][0][lane] = o0;
+    so[wave][1][lane] = o1;
+    if (g == 0) sml[wave][col] = make_float2(m, l);
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, sml[w][col].x);
+    l = 0.f;
+    o0 = o1 = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sml[w][col].x - m);
+      l += sml[w][col].y * f;
+      o0 += so[w][0][lane] * f;
+      o1 += so[w][1][lane] * f;
+    }
   }
   const int r = kv8_quotient(cc, a.by_G);
   if (cc < ncols) kv8_store(a.out + s * a.o_seq + r * a.o_row + (h * G + cc - r * G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
@@ -853,11 +873,13 @@ int launch_copy(hipStream_t s, K kernel, const Kv8CopyArgs& a) {
 
 template <int D, int JT, int NW, bool ONCE>
 int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
-  const int64_t units = (int64_t)a.c.n_seq * a.c.n_kv * p.chunks, grid = (units * p.runs + 7) / 8 * 8 * p.run_len;
-  hipLaunchKernelGGL((kv8_attn_kernel<D, JT, NW, ONCE>), dim3((unsigned)grid), dim3(NW * 64), 0, s, a);
+  const int64_t units = (int64_t)a.c.n_seq * a.c.n_kv * p.chunks, groups = (units * p.runs + 7) / 8 * 8 * p.run_len;
+  hipLaunchKernelGGL((kv8_attn_kernel<D, JT, NW, ONCE>), dim3((unsigned)groups), dim3(NW * 64), 0, s, a);
   BD_TRY(check_launch());
   if (p.chunks > 1) {
-    hipLaunchKernelGGL((kv8_merge_kernel<D>), dim3((unsigned)((int64_t)a.c.n_seq * a.c.n_kv * p.tiles * (D / 32))), dim3(64), 0, s, a, JT);
+    const dim3 grid((unsigned)((int64_t)a.c.n_seq * a.c.n_kv * p.tiles * (D / 32)));
+    if (p.chunks > 8) hipLaunchKernelGGL((kv8_merge_kernel<D, 4>), grid, dim3(256), 0, s, a, JT);
+    else hipLaunchKernelGGL((kv8_merge_kernel<D, 1>), grid, dim3(64), 0, s, a, JT);
     BD_TRY(check_launch());
   }
   return BD_OK;

@@ -94,9 +94,11 @@ struct Kv8Plan {
   int runs, run_len;     // parts of a unit's groups that go to an XCD each, and their length
   int64_t part_floats;   // workspace: unnormalised partial results, [sequence][kv head][tile][chunk]
 };
-constexpr int kv8_chunk_blocks = 32, kv8_cus = 256;
+constexpr int kv8_chunk_blocks = 16, kv8_least_blocks = 64, kv8_cus = 256;
 constexpr int64_t kv8_once_bytes = (int64_t)96 << 20;
 inline int64_t kv8_items(int n_seq, int M, int n_q, int n_kv) { return (int64_t)n_seq * n_kv * (((int64_t)M * (n_q / n_kv) + 15) / 16); }
+// Chunks for so many blocks, if there is room for them.
+__host__ __device__ inline int64_t kv8_parts(int64_t blocks) { return blocks < kv8_least_blocks ? 1 : (blocks + kv8_chunk_blocks / 2) / kv8_chunk_blocks; }
 inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_blocks, int window, int sinks) {
   Kv8Plan p{};
   p.tiles = (int)(((int64_t)M * (n_q / n_kv) + 15) / 16);
@@ -119,11 +121,11 @@ inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_bloc
   // Fewer items than CUs (stream: than two workgroups for each): the blocks of an item in chunks of about 32, as far as there are CUs for them.
   // us, 1 / 2 / 4 / 8 / 16 chunks: one row behind 8192 keys 30 / 21 / 15 / 11.9 / 11.7, behind 1024 8.5 / 10.3 / ..; 256 items behind 2048 keys
   // 12.2 / 18.0 / ..; 64 sequences up to 8192 in stream 52 / 36 / 33 / 42.
-  int64_t c = (blocks + kv8_chunk_blocks / 2) / kv8_chunk_blocks;
+  int64_t c = kv8_parts(blocks);
   const int64_t room = (once ? 2 : 1) * kv8_cus / items;
   if (c > room) c = room;
-  if (c > 64) c = 64;
-  p.chunks = c < 1 ? 1 : (int)c;
+  if (c > (once ? 128 : 64)) c = once ? 128 : 64;
+  p.chunks = c < 1 ? 1 : (int)c;                        // (no room for a second workgroup: 1)
   p.part_floats = p.chunks > 1 ? items * p.chunks * (16 * D + 32) : 0;
   const int64_t units = (int64_t)n_seq * n_kv * p.chunks;
   p.runs = units >= 8 ? 1 : (int)((8 + units - 1) / units);
@@ -133,8 +135,8 @@ inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_bloc
 }
 // Chunks that a group of `count` blocks really uses.
 __host__ __device__ inline int kv8_chunks_used(int count, int chunks) {
-  const int c = (count + kv8_chunk_blocks / 2) / kv8_chunk_blocks;
-  return c < 1 ? 1 : c < chunks ? c : chunks;
+  const int c = (int)kv8_parts(count);
+  return c < chunks ? c : chunks;
 }
 
 }  // namespace bd

@@ -375,6 +375,13 @@ def test_attention_on_a_long_cache(window, sinks):
     attend(rig, [random_heads(rng, 3, 8, 128), random_heads(rng, 1, 8, 128)], [40000, 9000], [3, 1], CAUSAL, window, sinks)
 
 
+@pytest.mark.parametrize("lens", [[300], [2600], [70001], [40000, 10, 3000]])
+def test_single_tokens_in_one_to_a_hundred_and_more_chunks(lens):
+    rng = np.random.default_rng(lens[0])
+    rig = filled(rng, [n + 1 for n in lens], 1, 64)
+    attend(rig, [random_heads(rng, 1, 8, 64) * 1.5 for _ in lens], lens, [1] * len(lens), CAUSAL)
+
+
 @pytest.mark.parametrize("n_seq,M,n_q,n,blocks", [(64, 8, 8, 17000, 540), (14, 40, 8, 8500, 270), (512, 1, 8, 8500, 400)])
 def test_more_blocks_than_a_wavefront_looks_up_at_once(n_seq, M, n_q, n, blocks):
     """Many sequences on the same pages, so long that every wavefront walks more than 64 blocks: one tile and eight wavefronts, two tiles and four, and one tile
