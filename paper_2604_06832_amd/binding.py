@@ -470,6 +470,8 @@ class Kv8Cache:
         """Attention of q [n_seq, M, n_q, D] (bfloat16) on the cache, to out (same shape).  workspace: a uint8 tensor of
         bd_k_kv8_attention_workspace bytes that nothing else uses while the call runs; None takes one from torch for this call."""
         shape, index, bf16 = q.shape, self.index, _torch.bfloat16
+        if window > 0x7FFFFFFF or sinks > 0x7FFFFFFF:
+            raise ValueError("window and sinks: below 2^31")
         if len(shape) != 4 or shape[0] != self.n_seq or q.dtype is not bf16 or out.dtype is not bf16 or out.shape != shape:
             raise ValueError(f"q and out: bfloat16 [{self.n_seq}, M, n_q, {self.D}], same shape")
         _, M, n_q, _ = shape

@@ -72,7 +72,9 @@ template <> __device__ inline u16 from_f32<u16>(float x) {
 // One wavefront per (block, head, keys or values), two blocks with heads of 64.  A lane has a patch of eight tokens (8 g ..) by eight dimensions:
 // rows move 16 bytes a lane and a token (256 or 128 contiguous bytes a row), and of the page the lane owns whole 16-byte pieces, the keys' after
 // an exchange with its neighbour, the values' after transposing bytes in registers.  Nothing crosses the wavefront: the
-// block's maximum is a reduction over its lanes.  Bound by the rows' bytes.
+// block's maximum is a reduction over its lanes.  Bound by the rows' bytes: eight prompts of up to 4096 rows (2 heads of 128, bf16) written and read
+// back 19.5 us, 80 MB (a copy of the same bytes 15.5); 16 contexts of up to 8000 read 37 us, 168 MB at 4.5 TB/s (a large copy 5.15); one block 4 us, its
+// launch.  Stores that pass the caches by, 23.5 for the first, and the keys' codes 16 bytes a lane bring nothing.
 struct Kv8CopyArgs {
   bd_kv8 c;
   Kv8Rows r;
@@ -401,7 +403,7 @@ __device__ inline void kv8_load_v(Kv8Block<D>& b, const uint4* p) {
 #pragma unroll
   for (int j = 0; j < D / 32; ++j) b.v[j] = kv8_load<ONCE>(p + (D / 32 + j) * 64);
 }
-// Eight codes times 2^e as a bf16 operand (exact).
+// Eight codes times 2^e as a bf16 operand (exact: four bits, and an exponent that bf16 has).
 __device__ inline bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
   union { bf16x8 v; bf16x2 h[4]; } o;
   o.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
@@ -546,11 +548,16 @@ __device__ inline void kv8_store(u16* o, const f32x4& a, const f32x4& b, float i
   *reinterpret_cast<uint4*>(o) = w.u;
 }
 
+// Softmax over a stream of blocks: O = sum 2^(s - m) v, L = sum 2^(s - m), both rescaled when m moves; O/L at the end.  Bound by the cache's
+// bytes where few rows read much (64 sequences up to 8192, 137 MB: 27.7 us without the joining kernel, 4.9 TB/s), and by the issue of vector instructions beside the
+// products where many rows do (1024 rows behind 7168 keys: 68 us, 64 GFLOP at 0.94 PFLOP/s; a large library product reaches 1.2): a block
+// costs a wavefront 34 products for two tiles, 64 conversions of pairs of codes and 16 exponentials.  A block of 32 rows behind 1024 keys 7.4 us, most of it
+// the launch and three dependent loads (page, scale, codes).
 // A workgroup of NW wavefronts takes JT tiles of a (sequence, kv head) and one of the chunks of their blocks: block number idx belongs to
 // chunk idx % chunks and in it to wavefront (idx / chunks) % NW.  The wavefronts merge through LDS; a group in one chunk stores its result, of several each
 // leaves an unnormalised partial, which kv8_merge_kernel sums in the order of the chunks.  The groups of a (sequence, kv head, chunk), which
 // read the same blocks, go to one XCD (numbers that differ by multiples of 8), where its L2 serves all but the first, or are dealt to several
-// where there are fewer than 8 such units; the last groups, which see most, start first.
+// where there are fewer than 8 such units (all of a unit on one XCD took four times as long for those 1024 rows); the last groups, which see most, start first.
 template <int D, int JT, int NW, bool ONCE>
 __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8AttnArgs a) {
   constexpr int DT = D / 16;
@@ -693,7 +700,8 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
 }
 
 // The chunks of a tile summed in their order: one wavefront per (sequence, kv head, tile, pair of d-tiles).  All it does is to wait for memory, so
-// the first eight partials are asked for before it is known how many there are (those that no group left are not looked at).
+// the first eight partials are asked for before it is known how many there are (those that no group left are not looked at): 3 us.  With more
+// than eight, four wavefronts take eight at a time in turn: 8 rows behind 32768 keys, 32 chunks, 13.4 instead of 15.7 us.
 template <int D, int W>
 __global__ __launch_bounds__(64 * W) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
   constexpr int P = 8, size = 16 * D + 32;
@@ -779,8 +787,9 @@ struct RopeArgs {
 };
 
 // A workgroup takes `per` rows: sines and cosines of their angles once for all heads (fp64 up to the reduced angle: at position 2^20 an
-// angle in fp32 is off by up to 2^-5), then the heads.  Bound by the rows' bytes: 16 a lane and access, VEC, where the two halves of a rotary part
-// fall on 16 bytes (with neighbouring pairs always), else an element at a time.
+// angle in fp32 is off by up to 2^-5), then the heads.  Bound by the rows' bytes, 16384 rows of 18 heads of 128 in fp32 63 us, 302 MB
+// at 4.8 TB/s: 16 a lane and access, VEC, where the two halves of a rotary part fall on 16 bytes (with neighbouring pairs always), else an element at a time
+// (70 us so).
 constexpr int kRopeRows = 4;
 __host__ __device__ inline int rope_item_log(int D, int N) { return (D == 128 ? 6 : 5) - (N == 8 ? 3 : N == 4 ? 2 : 0); }
 template <typename T, bool VEC>

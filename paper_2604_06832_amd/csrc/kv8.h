@@ -108,19 +108,21 @@ inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_bloc
     const int64_t w = ((int64_t)window + M + 62) / 32 + 1 + ((int64_t)sinks + 31) / 32;
     if (w < blocks) blocks = w;
   }
-  // One tile and a cache too large for the last-level cache: every block has one reader and will be gone from the caches before its next use, so
-  // its loads pass them by; four wavefronts, three workgroups a CU.  us, stream and walk: 64 sequences up to 8192 (137 MB) 35 and 40, 256 up to
-  // 4096 59 and 66; 32 up to 8192 (66 MB, which stays cached between runs) 27 and 21.  Loads alone take as long as the whole kernel.
+  // (Times in us, launches included, with the joining kernel where there is one.)
+  // One tile and page lists that may hold more than the last-level cache keeps from one step to the next: every block has one reader, so its loads
+  // pass the caches by; four wavefronts, three workgroups a CU.  Stream and walk, on caches that are cold: 64 sequences up to 8192 37 and 42, 256 up to
+  // 4096 59 and 66, 8 up to 32768 24.9 and 26.9, 32 up to 8192 24.0 and 25.3 (both 22.4 and 19.4 where they stay cached), 16 up to 8192 19.3 and 17.2.
   // More items than CUs: two tiles share each block that a wavefront loads and widens; four wavefronts, two workgroups a CU.
-  // Else one tile and eight wavefronts, for the shortest walk.  us, walk and wide: 256 items behind 2048 keys 13.2 and 18.1, 512 items 25.0
-  // and 21, 1024 rows (1024 items) behind 7168 keys 128 and 81 (four tiles 105).
+  // Else one tile and eight wavefronts, for the shortest walk.  Wide and walk: 256 items behind 2048 keys 17.7 and 13.2, 384 18.7 and 21.9, 512 20.2
+  // and 23.5, 1024 rows (1024 items) behind 7168 keys 81 and 115 (four tiles 105).
   const bool once = p.tiles == 1 && (int64_t)n_seq * n_kv * blocks * 64 * D >= kv8_once_bytes;
   p.form = once ? Kv8Form::stream : items > kv8_cus && p.tiles > 1 ? Kv8Form::wide : Kv8Form::walk;
   p.JT = p.form == Kv8Form::wide ? 2 : 1;
   p.groups = ceil_div(p.tiles, p.JT);
-  // Fewer items than CUs (stream: than two workgroups for each): the blocks of an item in chunks of about 32, as far as there are CUs for them.
-  // us, 1 / 2 / 4 / 8 / 16 chunks: one row behind 8192 keys 30 / 21 / 15 / 11.9 / 11.7, behind 1024 8.5 / 10.3 / ..; 256 items behind 2048 keys
-  // 12.2 / 18.0 / ..; 64 sequences up to 8192 in stream 52 / 36 / 33 / 42.
+  // Fewer items than CUs (stream: than two workgroups for each): the blocks of an item in chunks, as far as there are CUs for them.
+  // 1 / 2 / 4 / 8 / 16 chunks: one row behind 8192 keys 26.6 / 18.3 / 12.7 / 10.2 / 9.3, behind 2048 9.7 / 10.1 / 8.7, behind 1500 8.9 / 10.8, behind
+  // 1024 7.6 / 8.8 (the joining kernel costs 3); 256 items behind 2048 keys 10.7 / 16.7; 64 sequences up to 8192 in stream 52 / 37 / 34 / 43.  One row
+  // behind 262144 keys, 64 / 128 / 256 chunks: 38.8 / 32.9 / 38.1; behind 65536, 64 / 128: 14.8 / 17.2.
   int64_t c = kv8_parts(blocks);
   const int64_t room = (once ? 2 : 1) * kv8_cus / items;
   if (c > room) c = room;

@@ -1,5 +1,5 @@
 // Launch interface between the host translation unit (bd_lib.hip) and the translation units that hold the kernels
-// (k_stream.hip, k_mega.hip, k_prefill.hip, k_attention.hip): plain functions, so that the kernel files compile in
+// (k_stream.hip, k_mega.hip, k_prefill.hip, k_attention.hip, k_kv8.hip): plain functions, so that the kernel files compile in
 // parallel and none of them sees the context structure.
 #pragma once
 #include <hip/hip_runtime.h>

@@ -699,7 +699,7 @@ def test_binding_refuses_what_does_not_fit():
                  lambda: c.bd_k_kv8_write(k.half(), k.half()), lambda: c.bd_k_kv8_write(k.transpose(2, 3).contiguous().transpose(2, 3), k),
                  lambda: c.bd_k_kv8_write(k, k, rows=torch.zeros(2, device="cuda")), lambda: c.bd_k_kv8_write(k, k, rows=cuda_ints([1])),
                  lambda: c.bd_k_kv8_write(k.cpu(), k.cpu()), lambda: c.bd_k_kv8_read(None, k, k[:, :2]), lambda: c.bd_k_kv8_attention(q.float(), q.float(), CAUSAL),
-                 lambda: c.bd_k_kv8_attention(q, q[:, :2], CAUSAL), lambda: binding.bd_k_rope(binding.bd_k_rope_plan(64), q, cuda_ints([0])),
+                 lambda: c.bd_k_kv8_attention(q, q[:, :2], CAUSAL), lambda: c.bd_k_kv8_attention(q, torch.zeros_like(q), CAUSAL, window=2 ** 32 + 8), lambda: binding.bd_k_rope(binding.bd_k_rope_plan(64), q, cuda_ints([0])),
                  lambda: binding.bd_k_rope(binding.bd_k_rope_plan(128), q, cuda_ints([0, 0])),
                  lambda: binding.Kv8Cache(rig.codes, rig.scales[:1], rig.pages, rig.lens), lambda: binding.Kv8Cache(rig.codes, rig.scales, rig.pages, rig.lens[:1])):
         with pytest.raises(ValueError):
