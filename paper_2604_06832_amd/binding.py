@@ -356,23 +356,27 @@ def bd_k_attention_static(q, k, v, n_prefix: int, mode: int, out=None):
 # -- attention on a key/value cache in 8 bits (include/bd_kernels.h) --------------------------------------------------------
 # (A step makes these calls once a layer: what the checks and the call cost on the host counts, 4 to 5 us in all with the launch.)
 
-_torch = None
+_torch = _int32 = _bf16 = _dtypes = _current_device = _current_stream = None
 
 
 def _with_torch():
-    """torch, imported on first use."""
-    global _torch
+    """torch, imported on first use, and what of it every call needs."""
+    global _torch, _int32, _bf16, _dtypes, _current_device, _current_stream
     if _torch is None:
         import torch
+        _int32, _bf16, _dtypes = torch.int32, torch.bfloat16, {torch.bfloat16: BD_BF16, torch.float32: BD_F32}
+        _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         _torch = torch
     return _torch
 
 
-def _rows_of(t, name, heads, D, index):
-    """(pointer, stride between sequences, stride between rows) of a tensor of rows [n_seq, M, heads, D] on device `index`."""
-    shape = t.shape
+def _check_rows(shape, name, heads, D):
     if len(shape) != 4 or shape[2] != heads or shape[3] != D:
         raise ValueError(f"{name}: expected [n_seq, M, {heads}, {D}], got {list(shape)}")
+
+
+def _rows_of(t, name, heads, D, index):
+    """(pointer, stride between sequences, stride between rows) of a tensor of rows [n_seq, M, heads, D] (checked) on device `index`."""
     s0, s1, s2, s3 = t.stride()
     if s3 != 1 or (s2 != D and heads > 1) or t.get_device() != index:
         raise ValueError(f"{name}: heads and dimensions have to be contiguous, on cuda:{index}")
@@ -383,28 +387,25 @@ def _ints_of(t, name, n_seq, index):
     """Pointer of an int32 tensor with one number for each sequence; None passes NULL."""
     if t is None:
         return None
-    if t.dtype is not _torch.int32 or t.numel() != n_seq or t.get_device() != index or not t.is_contiguous():
+    if t.dtype is not _int32 or t.numel() != n_seq or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name}: expected {n_seq} int32 numbers on cuda:{index}")
     return t.data_ptr()
 
 
 def _dtype_of(t, name):
-    dtype = t.dtype
-    if dtype is _torch.bfloat16:
-        return BD_BF16
-    if dtype is _torch.float32:
-        return BD_F32
-    raise ValueError(f"{name}: bfloat16 or float32, got {dtype}")
+    dtype = _dtypes.get(t.dtype)
+    if dtype is None:
+        raise ValueError(f"{name}: bfloat16 or float32, got {t.dtype}")
+    return dtype
 
 
-def _enqueue(index, call, *args):
+def _enqueue(index, call, args):
     """call(stream, *args) on the current stream of device `index`."""
-    C_ = _torch._C
-    if C_._cuda_getDevice() == index:
-        code = call(C_._cuda_getCurrentRawStream(index), *args)
+    if _current_device() == index:
+        code = call(_current_stream(index), *args)
     else:
         with _torch.cuda.device(index):
-            code = call(C_._cuda_getCurrentRawStream(index), *args)
+            code = call(_current_stream(index), *args)
     if code < 0:
         raise BdError(code)
 
@@ -445,23 +446,22 @@ class Kv8Cache:
 
     def _pair(self, k, v, what):
         """Pointers and strides of keys and values, their type and M."""
-        index, shape = self.index, k.shape
-        kp = _rows_of(k, "keys", self.n_kv, self.D, index)
-        vp = _rows_of(v, "values", self.n_kv, self.D, index)
+        index, heads, D, shape = self.index, self.n_kv, self.D, k.shape
+        _check_rows(shape, "keys", heads, D)
         if shape[0] != self.n_seq or v.shape != shape or v.dtype is not k.dtype:
             raise ValueError(f"{what}: keys and values have the same shape, with {self.n_seq} sequences, and type")
-        return kp, vp, _dtype_of(k, "keys"), shape[1]
+        return _rows_of(k, "keys", heads, D, index), _rows_of(v, "values", heads, D, index), _dtype_of(k, "keys"), shape[1]
 
     def bd_k_kv8_write(self, k, v, rows=None):
         """Keys and values [n_seq, M, n_kv, D] (bfloat16 or float32) to positions lens ..."""
         kp, vp, dtype, M = self._pair(k, v, "bd_k_kv8_write")
-        _enqueue(self.index, self._write, self._p, *kp, *vp, dtype, M, _ints_of(rows, "rows", self.n_seq, self.index))
+        _enqueue(self.index, self._write, (self._p, *kp, *vp, dtype, M, _ints_of(rows, "rows", self.n_seq, self.index)))
 
     def bd_k_kv8_read(self, start, k_out, v_out, rows=None):
         """Positions start .. (None: from 0) as values, to k_out and v_out [n_seq, M, n_kv, D]."""
         kp, vp, dtype, M = self._pair(k_out, v_out, "bd_k_kv8_read")
-        _enqueue(self.index, self._read, self._p, _ints_of(start, "start", self.n_seq, self.index), M,
-                 _ints_of(rows, "rows", self.n_seq, self.index), dtype, *kp, *vp)
+        _enqueue(self.index, self._read, (self._p, _ints_of(start, "start", self.n_seq, self.index), M,
+                                          _ints_of(rows, "rows", self.n_seq, self.index), dtype, *kp, *vp))
 
     def bd_k_kv8_attention_workspace(self, n_q, M, window=0, sinks=0) -> int:
         return _check(self._workspace(self._p, n_q, M, window, sinks))
@@ -469,12 +469,14 @@ class Kv8Cache:
     def bd_k_kv8_attention(self, q, out, mode, window=0, sinks=0, scale=0.0, rows=None, workspace=None):
         """Attention of q [n_seq, M, n_q, D] (bfloat16) on the cache, to out (same shape).  workspace: a uint8 tensor of
         bd_k_kv8_attention_workspace bytes that nothing else uses while the call runs; None takes one from torch for this call."""
-        shape, index, bf16 = q.shape, self.index, _torch.bfloat16
+        shape, index, bf16 = q.shape, self.index, _bf16
         if window > 0x7FFFFFFF or sinks > 0x7FFFFFFF:
             raise ValueError("window and sinks: below 2^31")
         if len(shape) != 4 or shape[0] != self.n_seq or q.dtype is not bf16 or out.dtype is not bf16 or out.shape != shape:
             raise ValueError(f"q and out: bfloat16 [{self.n_seq}, M, n_q, {self.D}], same shape")
-        _, M, n_q, _ = shape
+        _, M, n_q, D = shape
+        if D != self.D:
+            raise ValueError(f"q: heads of {D}, the cache's are of {self.D}")
         qp, op = _rows_of(q, "q", n_q, self.D, index), _rows_of(out, "out", n_q, self.D, index)
         if workspace is None:
             wn = self._workspace(self._p, n_q, M, window, sinks)
@@ -483,7 +485,7 @@ class Kv8Cache:
         elif workspace.get_device() != index or not workspace.is_contiguous():
             raise ValueError(f"workspace: expected a contiguous tensor on cuda:{index}")
         wp, wn = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
-        _enqueue(index, self._attention, self._p, *qp, n_q, M, _ints_of(rows, "rows", self.n_seq, index), mode, window, sinks, scale, *op, wp, wn)
+        _enqueue(index, self._attention, (self._p, *qp, n_q, M, _ints_of(rows, "rows", self.n_seq, index), mode, window, sinks, scale, *op, wp, wn))
         return out
 
 
@@ -496,17 +498,18 @@ def bd_k_rope_plan(D, rotary_dim=None, layout=BD_ROPE_HALF, theta=1.0e6, scaling
 
 def bd_k_rope(plan, x, pos, out=None, rows=None):
     """The rows x [n_seq, M, heads, D] turned by their positions pos[s] + row, to out (None: a new tensor; x itself: in place)."""
-    torch = _torch or _with_torch()
+    if _torch is None:
+        _with_torch()
     shape, index = x.shape, x.get_device()
     if len(shape) != 4 or index < 0:
         raise ValueError(f"x: expected [n_seq, M, heads, D] on the GPU, got {list(shape)}")
     n, M, heads, D = shape
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device) if rows is None else torch.zeros(shape, dtype=x.dtype, device=x.device)
+        out = (_torch.empty if rows is None else _torch.zeros)(shape, dtype=x.dtype, device=x.device)
     elif out.shape != shape or out.dtype is not x.dtype:
         raise ValueError("x and out: same shape and type")
     if D != plan.D:
         raise ValueError(f"x: heads of {D}, the plan is for {plan.D}")
-    _enqueue(index, lib().bd_k_rope, C.addressof(plan), *_rows_of(x, "x", heads, D, index), *_rows_of(out, "out", heads, D, index), _dtype_of(x, "x"),
-             heads, n, M, _ints_of(pos, "pos", n, index), _ints_of(rows, "rows", n, index))
+    _enqueue(index, (_lib or lib()).bd_k_rope, (C.addressof(plan), *_rows_of(x, "x", heads, D, index), *_rows_of(out, "out", heads, D, index),
+                                                _dtype_of(x, "x"), heads, n, M, _ints_of(pos, "pos", n, index), _ints_of(rows, "rows", n, index)))
     return out
