@@ -20,8 +20,10 @@ struct Kv8Rows {          // a call's rows: their positions and how many of each
 __device__ inline bool kv8_take(const bd_kv8& c, const Kv8Rows& r, int s, int& first, int& rows) {
   first = 0;
   rows = r.M;
-  if (r.first != nullptr || r.rows != nullptr) {       // (both loads before a wait)
-    const int x = (r.first != nullptr ? r.first : r.rows)[s], y = (r.rows != nullptr ? r.rows : r.first)[s];
+  if (r.first != nullptr || r.rows != nullptr) {       // two scalar loads and one wait, whichever is given
+    typedef const __attribute__((address_space(4))) int* Ints;
+    int x = ((Ints)(r.first != nullptr ? r.first : r.rows))[s], y = ((Ints)(r.rows != nullptr ? r.rows : r.first))[s];
+    asm volatile("" : "+s"(x), "+s"(y));
     if (r.first != nullptr) first = x;
     if (r.rows != nullptr) rows = y;
   }
@@ -587,10 +589,9 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
   const int cnt = __builtin_amdgcn_readfirstlane(sp.count <= first ? 0 : used == 1 ? left / NW : left / step);
   // what there is to know of the wavefront's next 64 blocks, one a lane; a block whose page lies outside the pool, and one past the last, is
   // invisible to all, with the codes of page 0 for its own
-  uint32_t my_info, my_head;
+  uint32_t my_info, my_head, my_word;
   float my_ks, my_vs;
-  auto look_up = [&](int base) {
-    uint32_t word = 127u | 127u << 8 | kv8_v_nan;
+  auto ask = [&](int base) {                            // (page 0's own scales are asked for where there is no block, and not used)
     my_info = (uint32_t)kv8_nowhere | kv8_has_nan;
     my_head = (uint32_t)h;
     if (base + lane < cnt) {
@@ -600,17 +601,25 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
       const int page = kv8_in_pool(a.c, base == 0 && from_0 ? early : a.c.dev_pages[(size_t)s * a.c.max_blocks + kb]);
       if (page >= 0) {
         my_head = (uint32_t)page * (uint32_t)a.c.n_kv + (uint32_t)h;
-        word = a.c.dev_scales[my_head];
         const bool clear = sink ? kb < sp.clear_sinks : kb >= sp.clear_lo && kb < sp.clear_hi;
-        my_info = (uint32_t)kb | (clear ? kv8_clear : 0u) | ((word & kv8_v_nan) != 0u ? kv8_has_nan : 0u);
+        my_info = (uint32_t)kb | (clear ? kv8_clear : 0u);
       }
     }
-    my_ks = two_to(kv8_byte_exponent(word));
-    my_vs = two_to(kv8_byte_exponent(word >> 8));
+    my_word = a.c.dev_scales[my_head];
+  };
+  auto know = [&]() {
+    const bool there = (my_info & kv8_number) != (uint32_t)kv8_nowhere;
+    if (there && (my_word & kv8_v_nan) != 0u) my_info |= kv8_has_nan;
+    my_ks = two_to(there ? kv8_byte_exponent(my_word) : 0);
+    my_vs = two_to(there ? kv8_byte_exponent(my_word >> 8) : 0);
     // waited for here: behind a branch that may have left loads open, every later wait would be one for all of them
     asm volatile("" : "+v"(my_info), "+v"(my_head), "+v"(my_ks), "+v"(my_vs));
   };
-  look_up(0);
+  auto look_up = [&](int base) {
+    ask(base);
+    know();
+  };
+  ask(0);
   bf16x8 qf[JT][D / 32];
   f32x4 O[JT][DT], L[JT];
   float mrun[JT];
@@ -632,20 +641,25 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
     L[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
     mrun[jt] = kv8_lowest;
   }
+  auto codes_of = [&](int i) {
+    const uint32_t head = (uint32_t)__builtin_amdgcn_readlane((int)my_head, i & 63);
+    return reinterpret_cast<const uint4*>(a.c.dev_codes + (size_t)head * (64 * D)) + lane;
+  };
   auto block_of = [&](int i) {
     if ((i & 63) == 0 && i > 0) look_up(i);
-    const uint32_t head = (uint32_t)__builtin_amdgcn_readlane((int)my_head, i & 63);
     return Kv8Of{(uint32_t)__builtin_amdgcn_readlane((int)my_info, i & 63), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_ks), i & 63)),
                  __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_vs), i & 63)),
-                 reinterpret_cast<const uint4*>(a.c.dev_codes + (size_t)head * (64 * D)) + lane};
+                 codes_of(i)};
   };
   bool nan = false;
   if (cnt > 0) {
     Kv8Block<D> b;
-    Kv8Of of = block_of(0);
-    kv8_load_k<D, ONCE>(b, of.codes);
+    kv8_load_k<D, ONCE>(b, codes_of(0));                // (before the scales are there)
     __builtin_amdgcn_sched_barrier(0);                  // (in the order in which the loop will ask for them: its first wait has to hold for this entry to it too)
-    kv8_load_v<D, ONCE>(b, of.codes);
+    kv8_load_v<D, ONCE>(b, codes_of(0));
+    __builtin_amdgcn_sched_barrier(0);
+    know();
+    Kv8Of of = block_of(0);
     for (int i = 0; i < cnt; ++i) {
       const Kv8Of next = block_of(i + 1);
       kv8_step<D, JT, ONCE>(b, of, next, qf, O, mrun, L, cols, a, g);
