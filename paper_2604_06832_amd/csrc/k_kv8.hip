@@ -551,10 +551,10 @@ __device__ inline void kv8_store(u16* o, const f32x4& a, const f32x4& b, float i
 }
 
 // Softmax over a stream of blocks: O = sum 2^(s - m) v, L = sum 2^(s - m), both rescaled when m moves; O/L at the end.  Bound by the cache's
-// bytes where few rows read much (64 sequences up to 8192, 137 MB: 27.7 us without the joining kernel, 4.9 TB/s), and by the issue of vector instructions beside the
-// products where many rows do (1024 rows behind 7168 keys: 68 to 71 us, 64 GFLOP at 0.91 to 0.94 PFLOP/s; a large library product reaches 1.2): a block
-// costs a wavefront 34 products for two tiles, 64 conversions of pairs of codes and 16 exponentials.  A block of 32 rows behind 1024 keys 7.4 us, most of it
-// the launch and three dependent loads (page, scale, codes).
+// bytes where few rows read much (64 sequences up to 8192, 137 MB: 26.3 us without the joining kernel, 5.2 TB/s), and by the issue of vector instructions beside the
+// products where many rows do (1024 rows behind 7168 keys: 68 to 72 us, 64 GFLOP at 0.89 to 0.94 PFLOP/s; a large library product reaches 1.2): a block
+// costs a wavefront 34 products for two tiles, 64 conversions of pairs of codes and 16 exponentials.  A block of 32 rows behind 1024 keys 7.1 us, most of it
+// the launch and dependent loads (arguments, page and length, codes).
 // A workgroup of NW wavefronts takes JT tiles of a (sequence, kv head) and one of the chunks of their blocks: block number idx belongs to
 // chunk idx % chunks and in it to wavefront (idx / chunks) % NW.  The wavefronts merge through LDS; a group in one chunk stores its result, of several each
 // leaves an unnormalised partial, which kv8_merge_kernel sums in the order of the chunks.  The groups of a (sequence, kv head, chunk), which
