@@ -400,6 +400,27 @@ def test_more_blocks_than_a_wavefront_looks_up_at_once(n_seq, M, n_q, n, blocks)
     assert torch.equal(out, out[:1].expand_as(out)) and int(rig.status) == 0
 
 
+def test_the_last_positions_that_a_page_list_can_hold():
+    """Rows up to position 2^30 give the bits that they give at the start of a cache (a window's keys are all that either sees)."""
+    rng = np.random.default_rng(24)
+    codes, scales = torch.zeros((16, 2, 64 * 128), dtype=torch.uint8, device="cuda"), torch.zeros((16, 2), dtype=torch.int32, device="cuda")
+    status, outs, values = cuda_ints([0]), [], []
+    k, v, q = (torch.from_numpy(random_heads(rng, r, h, 128)).to(BF16).cuda()[None] for r, h in ((104, 2), (104, 2), (8, 16)))
+    for blocks, first in ((1 << 25, 2 ** 30 - 104), (8, 24)):
+        pages = torch.full((1, blocks), -1, dtype=torch.int32, device="cuda")
+        pages[0, first // 32:first // 32 + 4] = cuda_ints([3, 11, 0, 7])
+        lens = cuda_ints([first])
+        cache = binding.Kv8Cache(codes, scales, pages, lens, status)
+        cache.bd_k_kv8_write(k, v)
+        values.append(torch.zeros((2, 1, 104, 2, 128), device="cuda"))
+        cache.bd_k_kv8_read(lens, *values[-1])
+        lens += 96
+        outs.append(cache.bd_k_kv8_attention(q, torch.zeros_like(q), CAUSAL, window=64))
+        codes.zero_()
+    assert torch.equal(values[0], values[1]) and torch.equal(outs[0], outs[1])
+    assert bool(values[0].any()) and bool(outs[0].any()) and int(status) == 0
+
+
 def test_scores_far_apart_and_the_scale_argument():
     """Weights that are all but one, and maxima that move late: the largest scores at the end of the cache."""
     rng = np.random.default_rng(9)
