@@ -414,7 +414,14 @@ class Kv8Cache:
     """A key/value cache in 8 bits: caller's tensors behind one bd_kv8.  Methods carry the names of the C calls they wrap.
 
     codes uint8 [n_pages, n_kv, 64 D], scales int32 [n_pages, n_kv], pages int32 [n_seq, max_blocks], lens int32 [n_seq]
-    (positions held; moved on by the caller), status None or one int32.  The tensors are kept alive, and looked at when the kernels run."""
+    (positions held; moved on by the caller), status None or one int32.  The tensors are kept alive, and looked at when the kernels run: change
+    them in place (lens += rows, pages.copy_(...)).  The kernels and captured graphs hold their addresses, so another tensor in the place of one is refused;
+    for other tensors make another Kv8Cache."""
+
+    def __setattr__(self, name, value):
+        if self.__dict__.get(name, value) is not value:
+            raise AttributeError(f"Kv8Cache.{name} is fixed: change the tensor in place, or make another Kv8Cache")
+        object.__setattr__(self, name, value)
 
     def __init__(self, codes, scales, pages, lens, status=None):
         torch = _with_torch()

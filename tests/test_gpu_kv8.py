@@ -735,3 +735,17 @@ def test_binding_refuses_what_does_not_fit():
         with pytest.raises(binding.BdError) as e:
             call()
         assert e.value.code == code
+
+
+def test_lengths_move_on_in_place_and_are_not_replaced():
+    rig = filled(np.random.default_rng(25), [40, 40], 1, 64)
+    c, x = rig.cache, torch.ones((2, 1, 1, 64), device="cuda")
+    for name in ("codes", "scales", "pages", "lens", "status"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, getattr(c, name).clone())
+    rig.lens.fill_(20)
+    c.lens += 20                                                       # (the same tensor: the calls see it)
+    c.bd_k_kv8_write(x, x)
+    assert rig.lens.tolist() == [40, 40]
+    k, v = rig.read([40, 40], [1, 1])
+    assert (k == 1).all() and (v == 1).all()

@@ -88,3 +88,21 @@ def test_binding_takes_no_host_tensors():
         binding.Kv8Cache(torch.zeros((2, 1, 4096), dtype=torch.uint8), torch.zeros((2, 1), dtype=torch.int32), pages, lens)
     with pytest.raises(ValueError):
         binding.bd_k_rope(binding.bd_k_rope_plan(64), torch.zeros((1, 1, 1, 64)), lens)
+
+
+def test_a_cache_keeps_the_tensors_that_its_pointers_belong_to():
+    """Changing a tensor in place is fine; another tensor in its place is refused, since the kernels would go on with the old one's memory."""
+    c = binding.Kv8Cache.__new__(binding.Kv8Cache)
+    for name in ("codes", "scales", "pages", "lens", "status"):
+        t = torch.zeros(3, dtype=torch.int32)
+        setattr(c, name, t)
+        with pytest.raises(AttributeError):
+            setattr(c, name, t + 1)
+        with pytest.raises(AttributeError):
+            setattr(c, name, None)
+        assert getattr(c, name) is t
+    c.lens += 4
+    assert c.lens.tolist() == [4, 4, 4]
+    c.n_seq = 3
+    with pytest.raises(AttributeError):
+        c.n_seq = 2
