@@ -370,8 +370,18 @@ def _with_torch():
     return _torch
 
 
+# (a number past 32 bits would arrive as another one: ctypes cuts it without a word)
+_LEAST, _MOST = -0x80000000, 0x7FFFFFFF
+
+
+def _check_ints(**numbers):
+    for name, x in numbers.items():
+        if not _LEAST <= x <= _MOST:
+            raise ValueError(f"{name}: {x} is no 32-bit number")
+
+
 def _check_rows(shape, name, heads, D):
-    if len(shape) != 4 or shape[2] != heads or shape[3] != D:
+    if len(shape) != 4 or shape[2] != heads or shape[3] != D or shape[1] > _MOST:
         raise ValueError(f"{name}: expected [n_seq, M, {heads}, {D}], got {list(shape)}")
 
 
@@ -433,6 +443,7 @@ class Kv8Cache:
             raise ValueError(f"scales: expected a contiguous int32 tensor [{n_pages}, {n_kv}] on cuda:{index}")
         if pages.dtype != torch.int32 or pages.dim() != 2 or not pages.is_contiguous() or pages.get_device() != index:
             raise ValueError(f"pages: expected a contiguous int32 tensor [n_seq, max_blocks] on cuda:{index}")
+        _check_ints(n_seq=pages.shape[0], max_blocks=pages.shape[1])
         self.index, self.n_seq, self.n_kv, self.D = index, pages.shape[0], n_kv, size // 64
         if lens is None:
             raise ValueError("lens: expected one int32 for each sequence")
@@ -471,19 +482,20 @@ class Kv8Cache:
                                           _ints_of(rows, "rows", self.n_seq, self.index), dtype, *kp, *vp))
 
     def bd_k_kv8_attention_workspace(self, n_q, M, window=0, sinks=0) -> int:
+        _check_ints(n_q=n_q, M=M, window=window, sinks=sinks)
         return _check(self._workspace(self._p, n_q, M, window, sinks))
 
     def bd_k_kv8_attention(self, q, out, mode, window=0, sinks=0, scale=0.0, rows=None, workspace=None):
         """Attention of q [n_seq, M, n_q, D] (bfloat16) on the cache, to out (same shape).  workspace: a uint8 tensor of
         bd_k_kv8_attention_workspace bytes that nothing else uses while the call runs; None takes one from torch for this call."""
         shape, index, bf16 = q.shape, self.index, _bf16
-        if window > 0x7FFFFFFF or sinks > 0x7FFFFFFF:
-            raise ValueError("window and sinks: below 2^31")
+        if not (_LEAST <= window <= _MOST and _LEAST <= sinks <= _MOST and _LEAST <= mode <= _MOST):
+            _check_ints(window=window, sinks=sinks, mode=mode)
         if len(shape) != 4 or shape[0] != self.n_seq or q.dtype is not bf16 or out.dtype is not bf16 or out.shape != shape:
             raise ValueError(f"q and out: bfloat16 [{self.n_seq}, M, n_q, {self.D}], same shape")
         _, M, n_q, D = shape
-        if D != self.D:
-            raise ValueError(f"q: heads of {D}, the cache's are of {self.D}")
+        if D != self.D or M > _MOST:
+            raise ValueError(f"q: expected [{self.n_seq}, M, n_q, {self.D}], got {list(shape)}")
         qp, op = _rows_of(q, "q", n_q, self.D, index), _rows_of(out, "out", n_q, self.D, index)
         if workspace is None:
             wn = self._workspace(self._p, n_q, M, window, sinks)
@@ -499,7 +511,9 @@ class Kv8Cache:
 def bd_k_rope_plan(D, rotary_dim=None, layout=BD_ROPE_HALF, theta=1.0e6, scaling=BD_ROPE_PLAIN, factor=1.0, trained=1) -> bd_rope:
     """Plan of rotary positions (see include/bd_kernels.h); rotary_dim None: the whole head."""
     plan = bd_rope()
-    _check(lib().bd_k_rope_plan(C.addressof(plan), D, D if rotary_dim is None else rotary_dim, layout, theta, scaling, factor, trained))
+    rotary_dim = D if rotary_dim is None else rotary_dim
+    _check_ints(D=D, rotary_dim=rotary_dim, layout=layout, scaling=scaling, trained=trained)
+    _check(lib().bd_k_rope_plan(C.addressof(plan), D, rotary_dim, layout, theta, scaling, factor, trained))
     return plan
 
 
@@ -508,7 +522,7 @@ def bd_k_rope(plan, x, pos, out=None, rows=None):
     if _torch is None:
         _with_torch()
     shape, index = x.shape, x.get_device()
-    if len(shape) != 4 or index < 0:
+    if len(shape) != 4 or index < 0 or shape[0] > _MOST or shape[1] > _MOST:
         raise ValueError(f"x: expected [n_seq, M, heads, D] on the GPU, got {list(shape)}")
     n, M, heads, D = shape
     if out is None:

@@ -749,3 +749,15 @@ def test_lengths_move_on_in_place_and_are_not_replaced():
     assert rig.lens.tolist() == [40, 40]
     k, v = rig.read([40, 40], [1, 1])
     assert (k == 1).all() and (v == 1).all()
+
+
+def test_calls_refuse_numbers_past_32_bits():
+    rig = filled(np.random.default_rng(26), [40], 1, 64)
+    c, big = rig.cache, 1 << 32
+    x = torch.zeros((1, 1, 1, 64), dtype=BF16, device="cuda")
+    many = x.expand(1, big + 1, 1, 64)
+    for call in (lambda: c.bd_k_kv8_attention(x, torch.zeros_like(x), big), lambda: c.bd_k_kv8_attention(x, torch.zeros_like(x), CAUSAL, window=5 - big),
+                 lambda: c.bd_k_kv8_attention(x, torch.zeros_like(x), CAUSAL, window=5, sinks=4 - big), lambda: c.bd_k_kv8_attention(many, many, CAUSAL),
+                 lambda: c.bd_k_kv8_write(many, many), lambda: binding.bd_k_rope(binding.bd_k_rope_plan(64), many, cuda_ints([0]), out=many)):
+        with pytest.raises(ValueError):
+            call()

@@ -1,5 +1,6 @@
 """The 8-bit key/value cache and the rotary positions without a GPU: rules that host and device share (csrc/kv8.h) and refusals of the entry
 points under the sanitizers, the plan of the rotary positions against its formulas, and what the binding refuses."""
+import ctypes
 import math
 import os
 import shutil
@@ -106,3 +107,27 @@ def test_a_cache_keeps_the_tensors_that_its_pointers_belong_to():
     c.n_seq = 3
     with pytest.raises(AttributeError):
         c.n_seq = 2
+
+
+BIG = 1 << 32
+
+
+@pytest.mark.parametrize("change", [{"n_q": BIG + 4}, {"M": BIG + 4}, {"window": BIG + 8}, {"window": 8 - BIG}, {"sinks": BIG + 4}, {"sinks": 4 - BIG}])
+def test_workspace_refuses_numbers_past_32_bits(change):
+    """(ctypes would cut them to 32 bits and ask for another call's workspace.)"""
+    one = torch.zeros(64, dtype=torch.int32)
+    c = binding.Kv8Cache.__new__(binding.Kv8Cache)
+    c._c = binding.bd_kv8(one.data_ptr(), one.data_ptr(), one.data_ptr(), one.data_ptr(), None, 4, 2, 64, 2, 4096)
+    c._p, c._workspace = ctypes.addressof(c._c), binding.lib().bd_k_kv8_attention_workspace
+    call = {"n_q": 4, "M": 4, "window": 0, "sinks": 0}
+    assert c.bd_k_kv8_attention_workspace(**call) > 0
+    with pytest.raises(ValueError):
+        c.bd_k_kv8_attention_workspace(**{**call, **change})
+
+
+@pytest.mark.parametrize("change", [{"D": BIG + 64}, {"rotary_dim": BIG + 32}, {"layout": BIG}, {"layout": 1 - BIG}, {"scaling": BIG + 1}, {"trained": BIG + 4096}])
+def test_plan_refuses_numbers_past_32_bits(change):
+    call = {"D": 64, "rotary_dim": 32, "layout": 0, "scaling": binding.BD_ROPE_PARTS, "factor": 2.0, "trained": 4096}
+    binding.bd_k_rope_plan(**call)
+    with pytest.raises(ValueError):
+        binding.bd_k_rope_plan(**{**call, **change})
