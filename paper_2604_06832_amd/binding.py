@@ -116,11 +116,15 @@ def lib() -> C.CDLL:
 
 
 class BdError(RuntimeError):
-    def __init__(self, code: int):
+    """workspace: BD_E_CAPACITY of a call that has no cache of its own to exceed, whose text says what it needs."""
+
+    def __init__(self, code: int, workspace: bool = False):
         L = lib()
         msg = L.bd_strerror(code).decode()
         if code == BD_E_HIP:
             msg += ": " + L.bd_last_error().decode()
+        elif code == BD_E_CAPACITY and workspace:
+            msg = L.bd_last_error().decode()
         super().__init__(f"bd error {code}: {msg}")
         self.code = code
 
@@ -417,7 +421,7 @@ def _enqueue(index, call, args):
         with _torch.cuda.device(index):
             code = call(_current_stream(index), *args)
     if code < 0:
-        raise BdError(code)
+        raise BdError(code, workspace=True)
 
 
 class Kv8Cache:

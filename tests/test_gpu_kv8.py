@@ -761,3 +761,13 @@ def test_calls_refuse_numbers_past_32_bits():
                  lambda: c.bd_k_kv8_write(many, many), lambda: binding.bd_k_rope(binding.bd_k_rope_plan(64), many, cuda_ints([0]), out=many)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_a_short_workspace_says_so():
+    rig = filled(np.random.default_rng(27), [3000], 1, 64)
+    rig.lens.fill_(2999)
+    q = torch.zeros((1, 1, 4, 64), dtype=BF16, device="cuda")
+    size = rig.cache.bd_k_kv8_attention_workspace(4, 1)
+    with pytest.raises(binding.BdError, match=f"{size} bytes of workspace, got {size - 16}") as e:
+        rig.cache.bd_k_kv8_attention(q, torch.zeros_like(q), CAUSAL, workspace=torch.zeros(size - 16, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == binding.BD_E_CAPACITY and "capacity exceeded" not in str(e.value)

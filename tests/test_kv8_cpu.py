@@ -131,3 +131,15 @@ def test_plan_refuses_numbers_past_32_bits(change):
     binding.bd_k_rope_plan(**call)
     with pytest.raises(ValueError):
         binding.bd_k_rope_plan(**{**call, **change})
+
+
+def test_a_short_workspace_says_so_without_a_gpu(monkeypatch):
+    """(a refused call looks at no memory)"""
+    mem = torch.zeros(64, dtype=torch.int32)
+    p = mem.data_ptr() + -mem.data_ptr() % 16
+    c = binding.bd_kv8(p, p, p, p, None, 4, 2, 64, 2, 4096)
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    monkeypatch.setattr(binding, "_current_stream", lambda index: None)
+    with pytest.raises(binding.BdError, match="bytes of workspace, got 16") as e:
+        binding._enqueue(0, binding.lib().bd_k_kv8_attention, (ctypes.addressof(c), p, 1024, 256, 4, 4, None, binding.BD_MODE_CAUSAL, 0, 0, 0.0, p, 1024, 256, p, 16))
+    assert e.value.code == binding.BD_E_CAPACITY and "capacity exceeded" not in str(e.value)
