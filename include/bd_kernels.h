@@ -125,7 +125,7 @@ int bd_k_kv8_read(void* hip_stream, const bd_kv8* cache, const int32_t* dev_from
  * (bd_k_kv8_write before): out = softmax(scale q k) v over the keys a row sees, to dev_out (bf16).  Row r at position p = dev_len[s] + r sees key j
  * where j < dev_len[s] + rows, and j <= p with BD_MODE_CAUSAL (any j with BD_MODE_BIDIR), and, with window > 0, where
  * p - j < window or j < sinks: the last `window` positions and the first `sinks` ones (window 0: no window, sinks is then not looked at).
- * A row that sees no key (all of its pages lie outside the pool) becomes NaN.  scale > 0, or 0 for 1/sqrt(D); n_q 1 .. 65536 and
+ * A row that sees no key (all of its pages lie outside the pool) becomes NaN.  scale > 0 and at most 2^127, or 0 for 1/sqrt(D); n_q 1 .. 65536 and
  * n_seq n_kv ceil(M n_q / n_kv / 16) at most 2^22.  Products in bf16 (codes and queries exactly, the weights of the softmax rounded to it), sums and softmax in
  * fp32: scores, and values times 256 times the keys a row sees, have to stay below 2^127.
  * dev_workspace: bd_k_kv8_attention_workspace bytes (may be 0: NULL then), 16-byte aligned, free for others when the call has run;

@@ -971,7 +971,7 @@ extern "C" int bd_k_kv8_attention(void* hip_stream, const bd_kv8* cache, const v
   BD_TRY(check_attn(cache, n_q, M, window, sinks, false, &p));
   BD_TRY(check_rows(dev_q, BD_BF16, q_seq_stride, q_row_stride, cache->n_seq, M));
   BD_TRY(check_rows(dev_out, BD_BF16, out_seq_stride, out_row_stride, cache->n_seq, M, (int64_t)n_q * cache->D));
-  if (cache->dev_len == nullptr || (mode != BD_MODE_BIDIR && mode != BD_MODE_CAUSAL) || !(scale >= 0.f) || !std::isfinite(scale)) return BD_E_ARG;
+  if (cache->dev_len == nullptr || (mode != BD_MODE_BIDIR && mode != BD_MODE_CAUSAL) || !(scale >= 0.f && scale <= 0x1p127f)) return BD_E_ARG;     // (times log2 e finite)
   if (p.part_floats > 0 && (dev_workspace == nullptr || !aligned16(dev_workspace))) return BD_E_ARG;
   if (workspace_bytes < p.part_floats * 4) {
     set_last_error("bd_k_kv8_attention: this shape needs %lld bytes of workspace, got %lld", (long long)p.part_floats * 4, (long long)workspace_bytes);

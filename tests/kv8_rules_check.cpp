@@ -170,6 +170,7 @@ static void refusals() {
   for (int v : {0, -4, 5, 1 << 17}) { n_q = v; CHECK(attn(&c) == BD_E_ARG); } n_q = 4;
   for (int v : {0, (1 << 22) + 1}) { M = v; CHECK(attn(&c) == BD_E_ARG); } M = 4;
   for (float v : {-1.f, std::numeric_limits<float>::quiet_NaN(), std::numeric_limits<float>::infinity()}) { scale = v; CHECK(attn(&c) == BD_E_ARG); } scale = 0.f;
+  for (float v : {std::ldexp(1.f, 127) * 1.001f, 3e38f, std::numeric_limits<float>::max()}) { scale = v; CHECK(attn(&c) == BD_E_ARG); } scale = 0.f;      // (times log2 e infinite)
   M = 1 << 22; n_q = 8; CHECK(attn(&c) == BD_E_ARG); M = 4; n_q = 4;       // more tiles than a launch has room for
   {
     bd_kv8 many = c;

@@ -771,3 +771,9 @@ def test_a_short_workspace_says_so():
     with pytest.raises(binding.BdError, match=f"{size} bytes of workspace, got {size - 16}") as e:
         rig.cache.bd_k_kv8_attention(q, torch.zeros_like(q), CAUSAL, workspace=torch.zeros(size - 16, dtype=torch.uint8, device="cuda"))
     assert e.value.code == binding.BD_E_CAPACITY and "capacity exceeded" not in str(e.value)
+
+
+def test_the_largest_scale():
+    """Scores of 0 stay 0 (the scale times log2 e is finite): every visible value counts the same."""
+    rig = filled(np.random.default_rng(28), [100], 1, 64)
+    attend(rig, [np.zeros((4, 2, 64))], [96], [4], CAUSAL, scale=2.0 ** 127)
