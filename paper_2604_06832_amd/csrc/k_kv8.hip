@@ -582,7 +582,7 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
   if (c0 >= ncols) return;
   const int r0 = kv8_quotient(c0, a.by_G), r1 = kv8_quotient(min(c0 + JT * 16, ncols) - 1, a.by_G);
   const Kv8Span sp = kv8_span(n, rows, r0, r1, a.mode, a.window, a.sinks);
-  const int used = kv8_chunks_used(sp.count, a.chunks);
+  const int used = JT == 1 ? kv8_chunks_used(sp.count, a.chunks) : 1;     // (several tiles are taken where there is no room for chunks)
   if (chunk >= used) return;
   const int step = NW * used, first = wave * used + chunk;
   const int left = (sp.count - first + step - 1);
@@ -701,8 +701,8 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
     }
     if (used == 1) {
       if (cc < ncols) kv8_store(a.out + s * a.o_seq + r * a.o_row + (h * G + cc - r * G) * D + 32 * j + 8 * g, o0, o1, 1.f / l);
-    } else if (c0 + jt * 16 < ncols) {
-      float* pp = a.part + ((((int64_t)s * a.c.n_kv + h) * a.tiles + grp * JT + jt) * a.chunks + chunk) * (16 * D + 32);
+    } else if constexpr (JT == 1) {
+      float* pp = a.part + ((((int64_t)s * a.c.n_kv + h) * a.tiles + grp) * a.chunks + chunk) * (16 * D + 32);
       *reinterpret_cast<f32x4*>(pp + (2 * j * 64 + lane) * 4) = o0;
       *reinterpret_cast<f32x4*>(pp + ((2 * j + 1) * 64 + lane) * 4) = o1;
       if (j == 0 && g == 0) {
@@ -717,7 +717,7 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
 // the first eight partials are asked for before it is known how many there are (those that no group left are not looked at): 3 us.  With more
 // than eight, four wavefronts take eight at a time in turn: 8 rows behind 32768 keys, 32 chunks, 13.4 instead of 15.7 us.
 template <int D, int W>
-__global__ __launch_bounds__(64 * W) void kv8_merge_kernel(Kv8AttnArgs a, int JT) {
+__global__ __launch_bounds__(64 * W) void kv8_merge_kernel(Kv8AttnArgs a) {
   constexpr int P = 8, size = 16 * D + 32;
   const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
   const int j = blockIdx.x % (D / 32), item = blockIdx.x / (D / 32), sh = item / a.tiles, tile = item - sh * a.tiles;
@@ -738,9 +738,9 @@ __global__ __launch_bounds__(64 * W) void kv8_merge_kernel(Kv8AttnArgs a, int JT
   ask(wave * P);
   int n, rows;
   if (!kv8_take(a.c, a.r, s, n, rows)) return;
-  const int G = a.G, ncols = rows * G, c0 = tile / JT * JT * 16, cc = tile * 16 + col;
-  if (tile * 16 >= ncols) return;
-  const Kv8Span sp = kv8_span(n, rows, kv8_quotient(c0, a.by_G), kv8_quotient(min(c0 + JT * 16, ncols) - 1, a.by_G), a.mode, a.window, a.sinks);
+  const int G = a.G, ncols = rows * G, c0 = tile * 16, cc = c0 + col;
+  if (c0 >= ncols) return;
+  const Kv8Span sp = kv8_span(n, rows, kv8_quotient(c0, a.by_G), kv8_quotient(min(c0 + 16, ncols) - 1, a.by_G), a.mode, a.window, a.sinks);
   const int used = kv8_chunks_used(sp.count, a.chunks);
   if (used == 1) return;
   float m = kv8_lowest, l = 0.f;
@@ -905,9 +905,9 @@ template <int D, int JT, int NW, bool ONCE>
 int launch_attn(hipStream_t s, const Kv8AttnArgs& a, const Kv8Plan& p) {
   const int64_t units = (int64_t)a.c.n_seq * a.c.n_kv * p.chunks, groups = (units * p.runs + 7) / 8 * 8 * p.run_len;
   BD_TRY(launch(s, kv8_attn_kernel<D, JT, NW, ONCE>, dim3((unsigned)groups), NW * 64, a));
-  if (p.chunks > 1) {
+  if (JT == 1 && p.chunks > 1) {
     const dim3 grid((unsigned)((int64_t)a.c.n_seq * a.c.n_kv * p.tiles * (D / 32)));
-    BD_TRY(p.chunks > 8 ? launch(s, kv8_merge_kernel<D, 4>, grid, 256, a, JT) : launch(s, kv8_merge_kernel<D, 1>, grid, 64, a, JT));
+    BD_TRY(p.chunks > 8 ? launch(s, kv8_merge_kernel<D, 4>, grid, 256, a) : launch(s, kv8_merge_kernel<D, 1>, grid, 64, a));
   }
   return BD_OK;
 }

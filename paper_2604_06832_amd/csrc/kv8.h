@@ -1,7 +1,6 @@
 // The key/value cache in 8 bits (include/bd_kernels.h): layout of a page, arithmetic of its scales, rules on rows and on what a
 // row sees, and the plan of the attention's launch, shared by host and device.
 #pragma once
-#include <cstdlib>
 #include "../../include/bd_kernels.h"
 #include "common.h"
 

@@ -109,6 +109,7 @@ static void plan() {
     const Kv8Plan p = kv8_plan(n_seq, M, n_kv * G, n_kv, D, blocks, window, 4);
     CHECK(p.tiles * 16 >= M * G && (p.tiles - 1) * 16 < M * G && p.JT >= 1 && p.groups * p.JT >= p.tiles && (p.groups - 1) * p.JT < p.tiles);
     CHECK(p.chunks >= 1 && p.chunks <= (p.form == Kv8Form::stream ? 128 : 64));
+    CHECK(p.JT == 1 || p.chunks == 1);                       // (the joining kernel knows single tiles only)
     CHECK(p.runs >= 1 && p.runs * p.run_len >= p.groups && (p.runs == 1 || (int64_t)n_seq * n_kv * p.chunks < 8));
     // what the kernel makes of its number: every (unit, group) once
     const int64_t units = (int64_t)n_seq * n_kv * p.chunks, grid = (units * p.runs + 7) / 8 * 8 * p.run_len;
