@@ -777,3 +777,27 @@ def test_the_largest_scale():
     """Scores of 0 stay 0 (the scale times log2 e is finite): every visible value counts the same."""
     rig = filled(np.random.default_rng(28), [100], 1, 64)
     attend(rig, [np.zeros((4, 2, 64))], [96], [4], CAUSAL, scale=2.0 ** 127)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("layout", [binding.BD_ROPE_HALF, binding.BD_ROPE_INTERLEAVED])
+@pytest.mark.parametrize("D,R", [(64, 64), (64, 34), (128, 128), (128, 80), (128, 42)])
+def test_rope_of_many_rows_against_the_rotation_in_64_bits(D, R, layout, dtype):
+    """Several rows to a workgroup, its last one with three, one, two rows and all four; rotary parts whose halves fall on 16 bytes, and others."""
+    M, rows, pos = 1027, [1027, 1025, 1026, 1024], [0, 70001, 2 ** 30, 5]
+    x = torch.randn((4, M, 3, D), device="cuda").to(dtype)
+    plan = binding.bd_k_rope_plan(D, R, layout, 1e6, binding.BD_ROPE_PARTS, 4.0, 8192)
+    out = torch.full_like(x, 7.25)
+    binding.bd_k_rope(plan, x, cuda_ints(pos), out=out, rows=cuda_ints(rows))
+    for s in range(4):
+        n = rows[s]
+        src = x[s, :n].double().cpu().numpy()
+        want = plain_rope(src, pos[s], plan)
+        tol = rope_tolerance(want, src, dtype, plan.amplitude)
+        tol[..., R:] = 0.0
+        assert (np.abs(out[s, :n].double().cpu().numpy() - want) <= tol).all(), f"sequence {s}"
+        assert (out[s, n:] == 7.25).all()
+    y = x.clone()
+    binding.bd_k_rope(plan, y, cuda_ints(pos), out=y, rows=cuda_ints(rows))        # in place: the same
+    for s in range(4):
+        assert torch.equal(y[s, :rows[s]], out[s, :rows[s]]) and torch.equal(y[s, rows[s]:], x[s, rows[s]:])
