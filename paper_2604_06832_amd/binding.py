@@ -358,7 +358,7 @@ def bd_k_attention_static(q, k, v, n_prefix: int, mode: int, out=None):
 
 
 # -- attention on a key/value cache in 8 bits (include/bd_kernels.h) --------------------------------------------------------
-# (A step makes these calls once a layer: what the checks and the call cost on the host counts, 5 to 5.5 us in all, 2.5 of them the launch.)
+# (A step makes these calls once a layer: what the checks and the call cost on the host counts, 5 to 6 us in all, 2.5 of them the launch.)
 
 _torch = _int32 = _bf16 = _dtypes = _current_device = _current_stream = None
 

@@ -74,9 +74,10 @@ template <> __device__ inline u16 from_f32<u16>(float x) {
 // One wavefront per (block, head, keys or values), two blocks with heads of 64.  A lane has a patch of eight tokens (8 g ..) by eight dimensions:
 // rows move 16 bytes a lane and a token (256 or 128 contiguous bytes a row), and of the page the lane owns whole 16-byte pieces, the keys' after
 // an exchange with its neighbour, the values' after transposing bytes in registers.  Nothing crosses the wavefront: the
-// block's maximum is a reduction over its lanes.  Bound by the rows' bytes: eight prompts of up to 4096 rows (2 heads of 128, bf16) written and read
-// back 19.5 us, 80 MB (a copy of the same bytes 15.5); 16 contexts of up to 8000 read 37 us, 168 MB at 4.5 TB/s (a large copy 5.15); one block 4 us, its
-// launch.  Stores that pass the caches by, 23.5 for the first, and the keys' codes 16 bytes a lane bring nothing.
+// block's maximum is a reduction over its lanes.  Reading is bound by the rows' bytes: 16 contexts of up to 8000 rows (2 heads of
+// 128, bf16) 33.7 us, 168 MB at 5.0 TB/s (a large copy 5.15).  Eight prompts of up to 4096: read 8.7 us, 40 MB at 4.6 TB/s; written 11.5 us, 40 MB at 3.5 TB/s (a
+// copy of the same bytes 7.7): every wavefront is resident at once and loads, then reduces, then stores, so the first loads' 4 us are added whole.  One block
+// 3 us read, 4 us written, its launch.  Stores that pass the caches by (both together 23.5 us for 21.1 then) and the keys' codes 16 bytes a lane bring nothing.
 struct Kv8CopyArgs {
   bd_kv8 c;
   Kv8Rows r;
@@ -551,8 +552,9 @@ __device__ inline void kv8_store(u16* o, const f32x4& a, const f32x4& b, float i
 }
 
 // Softmax over a stream of blocks: O = sum 2^(s - m) v, L = sum 2^(s - m), both rescaled when m moves; O/L at the end.  Bound by the cache's
-// bytes where few rows read much (64 sequences up to 8192, 137 MB: 26.3 us without the joining kernel, 5.2 TB/s), and by the issue of vector instructions beside the
-// products where many rows do (1024 rows behind 7168 keys: 68 to 72 us, 64 GFLOP at 0.89 to 0.94 PFLOP/s; a large library product reaches 1.2): a block
+// bytes where few rows read much (64 sequences up to 8192, 137 MB: 26.4 us without the joining kernel, 5.2 TB/s; 24.8 where the last-level cache keeps them), and by the issue of
+// vector instructions beside the products where many rows do (1024 rows behind 7168 keys, 64 GFLOP: 67 us, 0.96 PFLOP/s, and 77 to 80 in the first
+// launches after a pause, before the clock has risen; a large library product reaches 1.2): a block
 // costs a wavefront 34 products for two tiles, 64 conversions of pairs of codes and 16 exponentials.  A block of 32 rows behind 1024 keys 7.1 us, most of it
 // the launch and dependent loads (arguments, page and length, codes).
 // A workgroup of NW wavefronts takes JT tiles of a (sequence, kv head) and one of the chunks of their blocks: block number idx belongs to
@@ -714,8 +716,8 @@ __global__ __launch_bounds__(NW * 64, JT == 1 ? 3 : 2) void kv8_attn_kernel(Kv8A
 }
 
 // The chunks of a tile summed in their order: one wavefront per (sequence, kv head, tile, pair of d-tiles).  All it does is to wait for memory, so
-// the first eight partials are asked for before it is known how many there are (those that no group left are not looked at): 3 us.  With more
-// than eight, four wavefronts take eight at a time in turn: 8 rows behind 32768 keys, 32 chunks, 13.4 instead of 15.7 us.
+// the first eight partials are asked for before it is known how many there are (those that no group left are not looked at): 3.5 to 4.5 us, 2.1 to 2.4 where
+// there is nothing to join.  With more than eight, four wavefronts take eight at a time in turn: 8 rows behind 32768 keys, 32 chunks, 12.3 instead of 14.6 us.
 template <int D, int W>
 __global__ __launch_bounds__(64 * W) void kv8_merge_kernel(Kv8AttnArgs a) {
   constexpr int P = 8, size = 16 * D + 32;
@@ -802,8 +804,8 @@ struct RopeArgs {
 
 // A workgroup takes `per` rows: sines and cosines of their angles once for all heads (fp64 up to the reduced angle: at position 2^20 an
 // angle in fp32 is off by up to 2^-5), then the heads.  Bound by the rows' bytes, 16384 rows of 18 heads of 128 in fp32 63 us, 302 MB
-// at 4.8 TB/s: 16 a lane and access, VEC, where the two halves of a rotary part fall on 16 bytes (with neighbouring pairs always), else an element at a time
-// (70 us so).
+// at 4.8 TB/s, in bf16 29 us, 151 MB at 5.2 TB/s: 16 a lane and access, VEC, where the two halves of a rotary part fall on 16 bytes (with neighbouring pairs
+// always), else an element at a time (a part of 66 of each head: 65 us in fp32, 44 in bf16).
 constexpr int kRopeRows = 4;
 __host__ __device__ inline int rope_item_log(int D, int N) { return (D == 128 ? 6 : 5) - (N == 8 ? 3 : N == 4 ? 2 : 0); }
 template <typename T, bool VEC>
@@ -1036,7 +1038,10 @@ extern "C" int bd_k_rope(void* hip_stream, const bd_rope* plan, const void* dev_
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int N = dtype == BD_F32 ? 4 : 8;
   const bool vec = plan->layout == BD_ROPE_INTERLEAVED || plan->rotary_dim % (2 * N) == 0;
-  const int per = (int64_t)M * n_seq >= 4096 ? kRopeRows : 1;               // few rows: a workgroup each
+  // Few rows: a workgroup each, for more lanes at work.  One / four rows a workgroup (18 heads of 128; us in a captured graph): 1024 rows 5.0 / 6.4 in bf16, 6.6 / 7.5
+  // in fp32, 2048 6.6 / 7.5 and 9.0 / 8.8, 4096 9.7 / 9.1 and 19.7 / 18.7, 8192 15.0 / 14.4 and 31.4 / 32.8, 16384 32.2 / 31.9 and 55.9 / 60.5 (so fp32 gains
+  // from four around 4096 rows only).
+  const int per = (int64_t)M * n_seq >= 4096 ? kRopeRows : 1;
   a.by_items = kv8_div(n_heads << rope_item_log(plan->D, vec ? N : 1));
   const dim3 grid(ceil_div(M, per), n_seq);
   if (dtype == BD_F32) return launch(s, vec ? rope_kernel<float, true> : rope_kernel<float, false>, grid, 256, a, per);

@@ -107,21 +107,25 @@ inline Kv8Plan kv8_plan(int n_seq, int M, int n_q, int n_kv, int D, int max_bloc
     const int64_t w = ((int64_t)window + M + 62) / 32 + 1 + ((int64_t)sinks + 31) / 32;
     if (w < blocks) blocks = w;
   }
-  // (Times in us, launches included, with the joining kernel where there is one.)
-  // One tile and page lists that may hold more than the last-level cache keeps from one step to the next: every block has one reader, so its loads
-  // pass the caches by; four wavefronts, three workgroups a CU.  Stream and walk, on caches that are cold: 64 sequences up to 8192 37 and 42, 256 up to
-  // 4096 59 and 66, 8 up to 32768 24.9 and 26.9, 32 up to 8192 24.0 and 25.3 (both 22.4 and 19.4 where they stay cached), 16 up to 8192 19.3 and 17.2.
+  // (Times in us of passes one after another in a captured graph, with the joining kernel where there is one, at the clock that lasting work runs at.
+  // Cold: other inputs from pass to pass, 500 MB in all; warm: the same ones, which the last-level cache keeps.)
+  // One tile and page lists with room for more than the last-level cache keeps from one step to the next: every block has one reader, so its loads
+  // pass the caches by; four wavefronts, three workgroups a CU.  Stream / walk, cold and warm: 64 sequences up to 8192 30.8 / 37.4 and 29.2 / 27.9, 8 up to
+  // 32768 21.0 / 23.2 and 19.2 / 19.7, 32 up to 8192 20.9 / 23.6 and 19.0 / 20.4, 256 up to 4096 50.5 / 57.8 cold; below the limit, 16 up to 8192,
+  // 14.1 / 15.0 and 13.0 / 12.2.  The lengths are on the device only, so it is the lists' room that counts, whatever the sequences hold.
   // More items than CUs: two tiles share each block that a wavefront loads and widens; four wavefronts, two workgroups a CU.
-  // Else one tile and eight wavefronts, for the shortest walk.  Wide and walk: 256 items behind 2048 keys 17.7 and 13.2, 384 18.7 and 21.9, 512 20.2
-  // and 23.5, 1024 rows (1024 items) behind 7168 keys 81 and 115 (four tiles 105).
+  // Else one tile and eight wavefronts, for the shortest walk.  Wide / walk: 256 items behind 2048 keys 16.3 / 11.2, 384 16.9 / 18.9, 512 17.5
+  // / 20.0, 1024 rows (1024 items) behind 7168 keys 68.6 / 95.2.
   const bool once = p.tiles == 1 && (int64_t)n_seq * n_kv * blocks * 64 * D >= kv8_once_bytes;
   p.form = once ? Kv8Form::stream : items > kv8_cus && p.tiles > 1 ? Kv8Form::wide : Kv8Form::walk;
   p.JT = p.form == Kv8Form::wide ? 2 : 1;
   p.groups = ceil_div(p.tiles, p.JT);
   // Fewer items than CUs (stream: than two workgroups for each): the blocks of an item in chunks, as far as there are CUs for them.
-  // 1 / 2 / 4 / 8 / 16 chunks: one row behind 8192 keys 26.6 / 18.3 / 12.7 / 10.2 / 9.3, behind 2048 9.7 / 10.1 / 8.7, behind 1500 8.9 / 10.8, behind
-  // 1024 7.6 / 8.8 (the joining kernel costs 3); 256 items behind 2048 keys 10.7 / 16.7; 64 sequences up to 8192 in stream 52 / 37 / 34 / 43.  One row
-  // behind 262144 keys, 64 / 128 / 256 chunks: 38.8 / 32.9 / 38.1; behind 65536, 64 / 128: 14.8 / 17.2.
+  // 1 / 2 / 4 / 8 / 16 chunks: one row behind 8192 keys 25.9 / 18.2 / 12.6 / 10.1 / 9.2, behind 2048 9.8 / 10.0 / 8.7, behind 1500 8.5 / 9.4, behind
+  // 1024 7.2 / 8.6, 32 rows behind 1024 7.6 / 9.0; 256 items behind 2048 keys 11.2 / 18.2; 64 sequences up to 8192 in stream 48.9 / 33.9 / 31.1 / 35.4 cold.  One
+  // row behind 262144 keys, 64 / 128 / 256 chunks: 33.0 / 30.2 / 35.5; behind 65536, 64 / 128: 13.9 / 16.4.
+  // Here too the lists' room counts: sequences far shorter than their lists use one chunk, but pay for the others' workgroups and the joining kernel.  Lists of
+  // 35 / 128 / 1024 pages: 32 rows behind 1024 keys 7.6 / 10.1 / 9.9, 8 sequences up to 1024 7.3 / 9.7 (256 pages) / 14.2 (stream).
   int64_t c = kv8_parts(blocks);
   const int64_t room = (once ? 2 : 1) * kv8_cus / items;
   if (c > room) c = room;
